@@ -471,6 +471,39 @@ spccl_status_t spccl_vr_all_reduce_sliced(void* const* send, void* const* recv, 
                                           void* scratch, uint64_t scratch_bytes,
                                           uint8_t* fmt_rs, uint8_t* fmt_ag, void* stream);
 
+/* ---- layer norm (a layer of the models whose gradients the collectives reduce) -- */
+
+/* y = (x - mean) * rstd * weight + bias over each row of a matrix of `rows`
+ * rows and `cols` columns (cols >= 1, both < 2^31), mean and 1 / sqrt(variance
+ * + eps) taken over the row (the biased variance).  ldx, ldy: elements between
+ * rows (>= cols).  x and y have `dtype`, weight and bias (NULL: ones, zeros)
+ * `wdtype`; sums are held in fp32 and y is rounded once.  mean and rstd
+ * (fp32, `rows` each, NULL: not wanted) are what the backward pass reads.
+ * y may be x itself (same pitch); no other overlap of an output. */
+spccl_status_t spccl_layer_norm(const void* x, uint64_t ldx, const void* weight, const void* bias, void* y, uint64_t ldy,
+                                float* mean, float* rstd, uint64_t rows, uint64_t cols, int32_t dtype, int32_t wdtype,
+                                double eps, void* stream);
+
+/* The gradients of a sum over dy * y: with h = (x - mean) * rstd and
+ * g = dy * weight,
+ *   dx = rstd * (g - avg(g) - h * avg(g * h))    (averages over the row),
+ *   dweight = sum over the rows of dy * h,  dbias = sum over the rows of dy.
+ * mean and rstd are the forward pass's.  dx (NULL: not wanted) has `dtype` and
+ * may be dy or x itself (same pitch).  dweight and dbias (either NULL: not
+ * wanted) have `gdtype`; with accumulate != 0 the sums are added to what is
+ * there, as a gradient bucket collects micro-batches, otherwise they replace
+ * it (zeros if rows == 0).  Sums over the rows are held in fp32 and their
+ * order depends on the sizes alone, so equal calls give equal bits.  scratch:
+ * spccl_layer_norm_scratch_bytes(rows, cols) bytes, 16-byte aligned, needed
+ * where dweight or dbias is wanted; it holds nothing between calls and is not
+ * a workspace of the other entry points. */
+uint64_t spccl_layer_norm_scratch_bytes(uint64_t rows, uint64_t cols);
+spccl_status_t spccl_layer_norm_backward(const void* dy, uint64_t lddy, const void* x, uint64_t ldx, const void* weight,
+                                         const float* mean, const float* rstd, void* dx, uint64_t lddx, void* dweight,
+                                         void* dbias, uint64_t rows, uint64_t cols, int32_t dtype, int32_t wdtype,
+                                         int32_t gdtype, int32_t accumulate, void* scratch, uint64_t scratch_bytes,
+                                         void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -43,7 +43,8 @@ EXPORTS = ("spccl_num_tiles", "spccl_pici_bytes", "spccl_stream_bound", "spccl_w
            "spccl_compress_coo", "spccl_slice_tracker_bytes", "spccl_compress_sliced_tracked",
            "spccl_reduce_sliced_tracked", "spccl_vr_sliced_scratch_bytes", "spccl_vr_reduce_scatter_sliced",
            "spccl_vr_all_gather_sliced", "spccl_vr_all_reduce_sliced", "spccl_compress_static",
-           "spccl_set_single_pass_limit")
+           "spccl_set_single_pass_limit", "spccl_layer_norm", "spccl_layer_norm_scratch_bytes",
+           "spccl_layer_norm_backward")
 
 
 class spccl_operand_t(ctypes.Structure):
@@ -119,6 +120,10 @@ _sigs = {
                                           _vp, _vp]),
     "spccl_vr_all_reduce_sliced": (_i32, [ctypes.POINTER(_vp), ctypes.POINTER(_vp), _i32, _u64, _i32,
                                           ctypes.POINTER(spccl_policy_t), _vp, _u64, _vp, _vp, _vp]),
+    "spccl_layer_norm": (_i32, [_vp, _u64, _vp, _vp, _vp, _u64, _vp, _vp, _u64, _u64, _i32, _i32, ctypes.c_double, _vp]),
+    "spccl_layer_norm_scratch_bytes": (_u64, [_u64, _u64]),
+    "spccl_layer_norm_backward": (_i32, [_vp, _u64, _vp, _u64, _vp, _vp, _vp, _vp, _u64, _vp, _vp, _u64, _u64, _i32, _i32,
+                                         _i32, _i32, _vp, _u64, _vp]),
 }
 for _name, (_res, _args) in _sigs.items():
     _f = getattr(_lib, _name)
@@ -431,6 +436,73 @@ def spccl_vr_all_reduce_sliced(send: list, recv: list, scratch: torch.Tensor, po
 def alloc_sliced(n: int, dtype: int, device="cuda") -> torch.Tensor:
     """A uint8 buffer with every slot of an n-element sliced stream."""
     return torch.empty(max(spccl_slice_count(n) * spccl_slice_bytes(dtype), 16), dtype=torch.uint8, device=device)
+
+
+# ---- layer norm ---------------------------------------------------------------------
+
+def _matrix(t: torch.Tensor, like: torch.Tensor | None, what: str) -> int:
+    """The row pitch of a matrix whose rows are contiguous, of the same shape
+    and dtype as `like`."""
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{what}: a matrix with contiguous rows is needed, got shape {tuple(t.shape)} strides {t.stride()}")
+    if like is not None and (t.shape != like.shape or t.dtype != like.dtype):
+        raise ValueError(f"{what}: {tuple(t.shape)} {t.dtype} does not match {tuple(like.shape)} {like.dtype}")
+    return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 1)
+
+
+def _vector(t: torch.Tensor | None, n: int, what: str, dtype=None) -> None:
+    if t is not None and (t.dim() != 1 or t.numel() != n or not (t.is_contiguous())
+                          or (dtype is not None and t.dtype != dtype)):
+        raise ValueError(f"{what}: {n} contiguous elements{f' of {dtype}' if dtype else ''} are needed, got "
+                         f"shape {tuple(t.shape)} {t.dtype}")
+
+
+def _dt_of_pair(a, b, otherwise: int, what: str) -> int:
+    given = [t for t in (a, b) if t is not None]
+    if len({t.dtype for t in given}) > 1:
+        raise ValueError(f"{what}: {given[0].dtype} and {given[1].dtype}")
+    return _dt(given[0]) if given else otherwise
+
+
+def spccl_layer_norm(x: torch.Tensor, weight: torch.Tensor | None, bias: torch.Tensor | None, y: torch.Tensor,
+                     mean: torch.Tensor | None = None, rstd: torch.Tensor | None = None, eps: float = 1e-5,
+                     stream=None) -> None:
+    """y = layer norm of x's rows; mean and rstd (fp32, one per row) are written
+    for the backward pass."""
+    ldx, ldy = _matrix(x, None, "x"), _matrix(y, x, "y")
+    rows, cols = x.shape
+    for t, n, what, dt in ((weight, cols, "weight", None), (bias, cols, "bias", None),
+                           (mean, rows, "mean", torch.float32), (rstd, rows, "rstd", torch.float32)):
+        _vector(t, n, what, dt)
+    _check(_lib.spccl_layer_norm(x.data_ptr(), ldx, _ptr_or_null(weight), _ptr_or_null(bias), y.data_ptr(), ldy,
+                                 _ptr_or_null(mean), _ptr_or_null(rstd), rows, cols, _dt(x),
+                                 _dt_of_pair(weight, bias, _dt(x), "weight and bias"), float(eps), _stream(stream)),
+           "spccl_layer_norm")
+
+
+def spccl_layer_norm_scratch_bytes(rows: int, cols: int) -> int:
+    return _lib.spccl_layer_norm_scratch_bytes(rows, cols)
+
+
+def spccl_layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: torch.Tensor | None, mean: torch.Tensor,
+                              rstd: torch.Tensor, dx: torch.Tensor | None, dweight: torch.Tensor | None,
+                              dbias: torch.Tensor | None, scratch: torch.Tensor | None = None,
+                              accumulate: bool = False, stream=None) -> None:
+    """The gradients of sum(dy * y): dx, and the weight's and the bias's (any
+    None: not wanted), added to what they hold if `accumulate`."""
+    ldx, lddy = _matrix(x, None, "x"), _matrix(dy, x, "dy")
+    lddx = 0 if dx is None else _matrix(dx, x, "dx")
+    rows, cols = x.shape
+    for t, n, what, dt in ((weight, cols, "weight", None), (dweight, cols, "dweight", None),
+                           (dbias, cols, "dbias", None), (mean, rows, "mean", torch.float32),
+                           (rstd, rows, "rstd", torch.float32)):
+        _vector(t, n, what, dt)
+    _check(_lib.spccl_layer_norm_backward(
+        dy.data_ptr(), lddy, x.data_ptr(), ldx, _ptr_or_null(weight), mean.data_ptr(), rstd.data_ptr(),
+        _ptr_or_null(dx), lddx, _ptr_or_null(dweight), _ptr_or_null(dbias), rows, cols, _dt(x),
+        _dt(x) if weight is None else _dt(weight), _dt_of_pair(dweight, dbias, SPCCL_F32, "dweight and dbias"),
+        1 if accumulate else 0, _ptr_or_null(scratch), 0 if scratch is None else _nbytes(scratch), _stream(stream)),
+        "spccl_layer_norm_backward")
 
 
 # ---- tensor helpers (allocation stays with the caller; these only size buffers) -----

@@ -1,0 +1,781 @@
+// Layer norm over the rows of a matrix, forward and backward, with the
+// reduction of the weight's and the bias's gradient over the rows.
+//
+//   forward    mean = sum x / C, rstd = 1 / sqrt(sum (x - mean)^2 / C + eps),
+//              y = (x - mean) rstd w + b
+//   backward   h = (x - mean) rstd, g = dy w:
+//              dx = rstd (g - sum g / C - h sum(g h) / C)
+//              dw = sum over rows of dy h,  db = sum over rows of dy
+//
+// Every sum is held in fp32; x, y and dx are rounded once, to their own type.
+// Both directions are bound by memory: forward reads x and writes y, backward
+// reads dy and x and writes dx, each once, so a row stays in the registers of
+// the lanes that loaded it between its statistics and its result.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <type_traits>
+
+#include "spccl_internal.h"
+#include "../../include/spccl.h"
+
+namespace spccl {
+namespace {
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
+// ---------------------------------------------------------------------------
+// element types: 16-byte vectors of either
+
+struct F32 {
+    using raw = uint32_t;
+    typedef u32x4 __attribute__((aligned(4))) vec_any;           // at any element's address
+    static constexpr int vec = 4;
+    static __device__ __forceinline__ float get(const u32x4& v, int j) { return __uint_as_float(v[j]); }
+    static __device__ __forceinline__ float one(raw r) { return __uint_as_float(r); }
+    static __device__ __forceinline__ raw round(float f) { return __float_as_uint(f); }
+    static __device__ __forceinline__ u32x4 pack(const float* f) {
+        return u32x4{__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])};
+    }
+};
+struct BF16 {
+    using raw = uint16_t;
+    typedef u32x4 __attribute__((aligned(2))) vec_any;
+    static constexpr int vec = 8;
+    static __device__ __forceinline__ float get(const u32x4& v, int j) {
+        return __uint_as_float(j & 1 ? v[j / 2] & 0xFFFF0000u : v[j / 2] << 16);
+    }
+    static __device__ __forceinline__ float one(raw r) { return __uint_as_float((uint32_t)r << 16); }
+    static __device__ __forceinline__ uint32_t two(float a, float b) {      // nearest, ties to even
+        return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, bf16x2));
+    }
+    static __device__ __forceinline__ raw round(float f) { return (raw)two(f, f); }
+    static __device__ __forceinline__ u32x4 pack(const float* f) {
+        return u32x4{two(f[0], f[1]), two(f[2], f[3]), two(f[4], f[5]), two(f[6], f[7])};
+    }
+};
+
+// A row's vector of `E::vec` elements from column c on, of which `rem` exist
+// (the others read 0).  Rows start at any element: the vector accesses ask
+// for no more than the element's alignment.
+template <class E>
+__device__ __forceinline__ u32x4 load_vec(const uint8_t* row, uint32_t c, uint32_t rem) {
+    using raw = typename E::raw;
+    const raw* p = reinterpret_cast<const raw*>(row) + c;
+    if (rem >= (uint32_t)E::vec) return *reinterpret_cast<const typename E::vec_any*>(p);
+    u32x4 v{0, 0, 0, 0};
+#pragma unroll
+    for (int j = 0; j < E::vec - 1; j++)
+        if ((uint32_t)j < rem) v[j * sizeof(raw) / 4] |= (uint32_t)p[j] << (8 * (j * sizeof(raw) % 4));
+    return v;
+}
+
+template <class E>
+__device__ __forceinline__ void store_vec(uint8_t* row, uint32_t c, uint32_t rem, const float* f) {
+    using raw = typename E::raw;
+    raw* p = reinterpret_cast<raw*>(row) + c;
+    if (rem >= (uint32_t)E::vec) {
+        *reinterpret_cast<typename E::vec_any*>(p) = E::pack(f);
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < E::vec - 1; j++)
+        if ((uint32_t)j < rem) p[j] = E::round(f[j]);
+}
+
+// N elements of a weight or bias from column c on (0 beyond `rem`, and
+// `absent` for a null array).
+template <class W, int N>
+__device__ __forceinline__ void load_param(const uint8_t* base, uint32_t c, uint32_t rem, float absent, float* f) {
+    if (!base) {
+#pragma unroll
+        for (int j = 0; j < N; j++) f[j] = absent;
+        return;
+    }
+    if constexpr (N >= W::vec) {
+#pragma unroll
+        for (int h = 0; h < N / W::vec; h++) {
+            const uint32_t at = h * W::vec;
+            const u32x4 v = load_vec<W>(base, c + at, rem > at ? rem - at : 0);
+#pragma unroll
+            for (int j = 0; j < W::vec; j++) f[h * W::vec + j] = W::get(v, j);
+        }
+    } else {                                              // fp32 rows, bf16 weights: half a vector
+        static_assert(N * 2 == W::vec, "half a vector");
+        typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+        typedef u32x2 __attribute__((aligned(2))) halfu;
+        const uint16_t* p = reinterpret_cast<const uint16_t*>(base) + c;
+        if (rem >= (uint32_t)N) {
+            const u32x2 v = *reinterpret_cast<const halfu*>(p);
+#pragma unroll
+            for (int j = 0; j < N; j++) f[j] = __uint_as_float(j & 1 ? v[j / 2] & 0xFFFF0000u : v[j / 2] << 16);
+        } else {
+#pragma unroll
+            for (int j = 0; j < N; j++) f[j] = (uint32_t)j < rem ? W::one(p[j]) : 0.f;
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------
+// sums over the lanes of a row
+
+template <int Ctrl>
+__device__ __forceinline__ float dpp(float x) {
+    return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), Ctrl, 0xf, 0xf, true));
+}
+__device__ __forceinline__ float lane_of(float x, int lane) {
+    return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(x), lane));
+}
+
+// The sum over groups of L consecutive lanes, in every lane of the group:
+// partners at distance 1 and 2 (quad permutations), then the mirrored lane of
+// 8 and of 16 (whose quads and halves hold one value by then), then the four
+// rows of 16.
+template <int L>
+__device__ __forceinline__ float lanes_sum(float x) {
+    constexpr int kXor1 = 0xB1, kXor2 = 0x4E, kMirror8 = 0x141, kMirror16 = 0x140;
+    x += dpp<kXor1>(x);
+    x += dpp<kXor2>(x);
+    x += dpp<kMirror8>(x);
+    if constexpr (L >= 16) x += dpp<kMirror16>(x);
+    if constexpr (L == 32) x += __shfl_xor(x, 16);
+    if constexpr (L == 64) x = (lane_of(x, 0) + lane_of(x, 16)) + (lane_of(x, 32) + lane_of(x, 48));
+    return x;
+}
+
+// How a row lies over lanes: L lanes of one wave (Waves = 1) or all lanes of
+// Waves waves, K vectors each; vector k of lane i is vector k * lanes + i.
+template <class E, int L, int Waves, int K>
+struct Row {
+    static_assert(Waves == 1 || L == 64, "a row is part of a wave, or whole waves");
+    static constexpr uint32_t lanes = L * Waves;
+    static constexpr uint32_t cap = lanes * K * E::vec;           // columns that fit
+    static constexpr uint32_t threads = Waves > 4 ? 64 * Waves : 256;
+    static constexpr uint32_t rows = threads / lanes;             // rows of a block at a time
+    static constexpr uint32_t waves = threads / 64;
+};
+
+struct LnArgs {
+    const uint8_t* x;
+    const uint8_t* w;
+    const uint8_t* b;
+    uint8_t* y;
+    float* mean;
+    float* rstd;
+    uint64_t ldx, ldy;        // bytes between rows
+    uint64_t rows;
+    uint32_t cols;
+    float eps;
+};
+
+// One row per group of lanes.  The deviations are summed about the mean in a
+// second pass over the registers, so a large mean costs no precision; where a
+// row spans waves, each takes the mean and the squared deviations of its own
+// columns and the waves' are joined (n1 m1 + n2 m2; the squared distance of a
+// part's mean from the whole's counts for each of its columns), so a row
+// meets one barrier.
+template <class E, class W, int L, int Waves, int K>
+__global__ void __launch_bounds__((Row<E, L, Waves, K>::threads)) k_layer_norm(LnArgs g) {
+    using R = Row<E, L, Waves, K>;
+    constexpr int V = E::vec;
+    const uint32_t i = threadIdx.x % R::lanes;                    // lane of the row
+    const uint32_t group = threadIdx.x / R::lanes;
+    const uint64_t row = (uint64_t)blockIdx.x * R::rows + group;
+    const bool mine = row < g.rows;
+    const uint8_t* src = g.x + (mine ? row : 0) * g.ldx;
+    u32x4 v[K];
+#pragma unroll
+    for (int k = 0; k < K; k++) {
+        const uint32_t c = (k * R::lanes + i) * V;
+        const uint32_t rem = mine && c < g.cols ? g.cols - c : 0;
+        v[k] = load_vec<E>(src, c, rem);
+    }
+    float sum = 0.f;
+#pragma unroll
+    for (int k = 0; k < K; k++)
+#pragma unroll
+        for (int j = 0; j < V; j++) sum += E::get(v[k], j);
+    // the columns whose mean is taken first: the row's, or this wave's part
+    uint32_t n = g.cols;
+    if constexpr (Waves > 1) {
+        n = 0;
+#pragma unroll
+        for (int k = 0; k < K; k++) {
+            const uint32_t c0 = (k * R::lanes + (i & ~63u)) * V;
+            n += c0 < g.cols ? (g.cols - c0 < 64u * V ? g.cols - c0 : 64u * V) : 0;
+        }
+    }
+    float mean = lanes_sum<L>(sum) / (float)(n ? n : 1);
+    float dev = 0.f;
+#pragma unroll
+    for (int k = 0; k < K; k++) {
+        const uint32_t c = (k * R::lanes + i) * V;
+        const uint32_t rem = c < g.cols ? g.cols - c : 0;
+        if (rem >= (uint32_t)V) {
+#pragma unroll
+            for (int j = 0; j < V; j++) {
+                const float d = E::get(v[k], j) - mean;
+                dev = fmaf(d, d, dev);
+            }
+        } else if (rem) {
+#pragma unroll
+            for (int j = 0; j < V - 1; j++) {
+                const float d = (uint32_t)j < rem ? E::get(v[k], j) - mean : 0.f;
+                dev = fmaf(d, d, dev);
+            }
+        }
+    }
+    dev = lanes_sum<L>(dev);
+    if constexpr (Waves > 1) {
+        __shared__ float s_n[R::waves], s_mean[R::waves], s_dev[R::waves];
+        const uint32_t wave = threadIdx.x >> 6;
+        if ((threadIdx.x & 63u) == 0) {
+            s_n[wave] = (float)n;
+            s_mean[wave] = mean;
+            s_dev[wave] = dev;
+        }
+        __syncthreads();
+        const uint32_t first = group * Waves;
+        float total = 0.f;
+#pragma unroll
+        for (int q = 0; q < Waves; q++) total += s_n[first + q] * s_mean[first + q];
+        mean = total / (float)g.cols;
+        dev = 0.f;
+#pragma unroll
+        for (int q = 0; q < Waves; q++) {
+            const float d = s_mean[first + q] - mean;
+            dev += fmaf(s_n[first + q], d * d, s_dev[first + q]);
+        }
+    }
+    if (!mine) return;
+    const float rstd = 1.0f / sqrtf(dev / (float)g.cols + g.eps);
+    if (i == 0) {
+        if (g.mean) g.mean[row] = mean;
+        if (g.rstd) g.rstd[row] = rstd;
+    }
+    uint8_t* dst = g.y + row * g.ldy;
+#pragma unroll
+    for (int k = 0; k < K; k++) {
+        const uint32_t c = (k * R::lanes + i) * V;
+        if (c >= g.cols) break;
+        const uint32_t rem = g.cols - c;
+        float w[V], b[V], y[V];
+        load_param<W, V>(g.w, c, rem, 1.f, w);
+        load_param<W, V>(g.b, c, rem, 0.f, b);
+#pragma unroll
+        for (int j = 0; j < V; j++) y[j] = fmaf((E::get(v[k], j) - mean) * rstd, w[j], b[j]);
+        store_vec<E>(dst, c, rem, y);
+    }
+}
+
+// Rows too long for the registers of a block: the block reads its row three
+// times (its L2 holds it from the first), for the mean, the deviations and y.
+template <class E, class W>
+__global__ void __launch_bounds__(1024) k_layer_norm_long(LnArgs g) {
+    constexpr int V = E::vec;
+    __shared__ float s_part[2][16];
+    const uint8_t* src = g.x + (uint64_t)blockIdx.x * g.ldx;
+    uint8_t* dst = g.y + (uint64_t)blockIdx.x * g.ldy;
+    const uint32_t wave = threadIdx.x >> 6;
+    const auto block_sum = [&](float x, int which) {
+        x = lanes_sum<64>(x);
+        if ((threadIdx.x & 63u) == 0) s_part[which][wave] = x;
+        __syncthreads();
+        float t = 0.f;
+#pragma unroll
+        for (int q = 0; q < 16; q++) t += s_part[which][q];
+        return t;
+    };
+    float sum = 0.f;
+    for (uint32_t c = threadIdx.x * V; c < g.cols; c += 1024 * V) {
+        const u32x4 v = load_vec<E>(src, c, g.cols - c);
+#pragma unroll
+        for (int j = 0; j < V; j++) sum += E::get(v, j);
+    }
+    const float mean = block_sum(sum, 0) / (float)g.cols;
+    float dev = 0.f;
+    for (uint32_t c = threadIdx.x * V; c < g.cols; c += 1024 * V) {
+        const uint32_t rem = g.cols - c;
+        const u32x4 v = load_vec<E>(src, c, rem);
+#pragma unroll
+        for (int j = 0; j < V; j++) {
+            const float d = (uint32_t)j < rem ? E::get(v, j) - mean : 0.f;
+            dev = fmaf(d, d, dev);
+        }
+    }
+    const float rstd = 1.0f / sqrtf(block_sum(dev, 1) / (float)g.cols + g.eps);
+    if (threadIdx.x == 0) {
+        if (g.mean) g.mean[blockIdx.x] = mean;
+        if (g.rstd) g.rstd[blockIdx.x] = rstd;
+    }
+    for (uint32_t c = threadIdx.x * V; c < g.cols; c += 1024 * V) {
+        const uint32_t rem = g.cols - c;
+        const u32x4 v = load_vec<E>(src, c, rem);
+        float w[V], b[V], y[V];
+        load_param<W, V>(g.w, c, rem, 1.f, w);
+        load_param<W, V>(g.b, c, rem, 0.f, b);
+#pragma unroll
+        for (int j = 0; j < V; j++) y[j] = fmaf((E::get(v, j) - mean) * rstd, w[j], b[j]);
+        store_vec<E>(dst, c, rem, y);
+    }
+}
+
+// ---------------------------------------------------------------------------
+// backward
+
+struct LnBackArgs {
+    const uint8_t* dy;
+    const uint8_t* x;
+    const uint8_t* w;
+    const float* mean;
+    const float* rstd;
+    uint8_t* dx;              // null: only the weight's and bias's gradient
+    float* part;              // [blocks][2][cols]: the blocks' sums of dy h and of dy (null: not wanted)
+    uint64_t lddy, ldx, lddx; // bytes between rows
+    uint64_t rows;
+    uint32_t cols;
+};
+
+// Each group of lanes walks over rows, keeping its columns' sums of dy h and
+// dy in registers; a block joins its groups' through LDS, in their order, and
+// leaves one pair of sums per column for k_layer_norm_grads, so no sum depends
+// on which block comes first.
+template <class E, class W, int L, int Waves, int K>
+__global__ void __launch_bounds__((Row<E, L, Waves, K>::threads)) k_layer_norm_back(LnBackArgs g) {
+    using R = Row<E, L, Waves, K>;
+    constexpr int V = E::vec;
+    __shared__ float s_sum[R::rows > 1 ? R::cap : 1];
+    __shared__ float s_row[2][2][R::waves];
+    const uint32_t i = threadIdx.x % R::lanes;
+    const uint32_t group = threadIdx.x / R::lanes;
+    const uint32_t wave = threadIdx.x >> 6;
+    float dw[K][V], db[K][V];
+#pragma unroll
+    for (int k = 0; k < K; k++)
+#pragma unroll
+        for (int j = 0; j < V; j++) dw[k][j] = db[k][j] = 0.f;
+    const float inv = 1.0f / (float)g.cols;
+    uint32_t turn = 0;
+    for (uint64_t r0 = (uint64_t)blockIdx.x * R::rows; r0 < g.rows; r0 += (uint64_t)gridDim.x * R::rows, turn ^= 1) {
+        const uint64_t row = r0 + group;
+        const bool mine = row < g.rows;
+        const uint64_t at = mine ? row : 0;
+        const uint8_t* px = g.x + at * g.ldx;
+        const uint8_t* pdy = g.dy + at * g.lddy;
+        u32x4 x[K], dy[K];
+#pragma unroll
+        for (int k = 0; k < K; k++) {
+            const uint32_t c = (k * R::lanes + i) * V;
+            const uint32_t rem = mine && c < g.cols ? g.cols - c : 0;
+            x[k] = load_vec<E>(px, c, rem);
+            dy[k] = load_vec<E>(pdy, c, rem);
+        }
+        const float mean = mine ? g.mean[at] : 0.f, rstd = mine ? g.rstd[at] : 0.f;
+        // an opaque column: the weight is read again for each row (it stays in
+        // the caches) instead of held in registers over all of them
+        uint32_t ci = i * V;
+        asm volatile("" : "+v"(ci));
+        float s1 = 0.f, s2 = 0.f;
+#pragma unroll
+        for (int k = 0; k < K; k++) {
+            const uint32_t c = k * R::lanes * V + ci;
+            float w[V];
+            load_param<W, V>(g.w, c, c < g.cols ? g.cols - c : 0, 1.f, w);
+#pragma unroll
+            for (int j = 0; j < V; j++) {
+                const float d = E::get(dy[k], j);
+                const float h = (E::get(x[k], j) - mean) * rstd;
+                const float t = d * w[j];
+                s1 = fmaf(t, h, s1);
+                s2 += t;
+                dw[k][j] = fmaf(d, h, dw[k][j]);
+                db[k][j] += d;
+            }
+        }
+        if (!g.dx) continue;
+        s1 = lanes_sum<L>(s1);
+        s2 = lanes_sum<L>(s2);
+        if constexpr (Waves > 1) {
+            // two buffers in turn: a wave that is a row ahead writes the other
+            if ((threadIdx.x & 63u) == 0) {
+                s_row[turn][0][wave] = s1;
+                s_row[turn][1][wave] = s2;
+            }
+            __syncthreads();
+            s1 = s2 = 0.f;
+#pragma unroll
+            for (int q = 0; q < Waves; q++) {
+                s1 += s_row[turn][0][group * Waves + q];
+                s2 += s_row[turn][1][group * Waves + q];
+            }
+        }
+        s1 *= inv;
+        s2 *= inv;
+        if (!mine) continue;
+        uint8_t* dst = g.dx + row * g.lddx;
+#pragma unroll
+        for (int k = 0; k < K; k++) {
+            const uint32_t c = k * R::lanes * V + ci;
+            if (c >= g.cols) break;
+            float w[V], o[V];
+            load_param<W, V>(g.w, c, g.cols - c, 1.f, w);
+#pragma unroll
+            for (int j = 0; j < V; j++) {
+                const float h = (E::get(x[k], j) - mean) * rstd;
+                o[j] = fmaf(-h, s1, fmaf(E::get(dy[k], j), w[j], -s2)) * rstd;
+            }
+            store_vec<E>(dst, c, g.cols - c, o);
+        }
+    }
+    if (!g.part) return;
+    float* part = g.part + (uint64_t)blockIdx.x * 2 * g.cols;
+#pragma unroll
+    for (int which = 0; which < 2; which++) {
+        float(&acc)[K][V] = which ? db : dw;
+        if constexpr (R::rows > 1) {
+            for (uint32_t q = 0; q < R::rows; q++) {
+                __syncthreads();
+                if (group == q) {
+#pragma unroll
+                    for (int k = 0; k < K; k++)
+#pragma unroll
+                        for (int j = 0; j < V; j++) {
+                            const uint32_t c = (k * R::lanes + i) * V + j;
+                            s_sum[c] = q ? s_sum[c] + acc[k][j] : acc[k][j];
+                        }
+                }
+            }
+            __syncthreads();
+            for (uint32_t c = threadIdx.x; c < g.cols; c += R::threads) part[which * g.cols + c] = s_sum[c];
+        } else {
+#pragma unroll
+            for (int k = 0; k < K; k++)
+#pragma unroll
+                for (int j = 0; j < V; j++) {
+                    const uint32_t c = (k * R::lanes + i) * V + j;
+                    if (c < g.cols) part[which * g.cols + c] = acc[k][j];
+                }
+        }
+    }
+}
+
+// Long rows: dx of one row per block, reading the row twice.
+template <class E, class W>
+__global__ void __launch_bounds__(1024) k_layer_norm_back_long(LnBackArgs g) {
+    constexpr int V = E::vec;
+    __shared__ float s_part[2][16];
+    const uint64_t row = blockIdx.x;
+    const uint8_t* px = g.x + row * g.ldx;
+    const uint8_t* pdy = g.dy + row * g.lddy;
+    const float mean = g.mean[row], rstd = g.rstd[row];
+    float s1 = 0.f, s2 = 0.f;
+    for (uint32_t c = threadIdx.x * V; c < g.cols; c += 1024 * V) {
+        const uint32_t rem = g.cols - c;
+        const u32x4 x = load_vec<E>(px, c, rem), dy = load_vec<E>(pdy, c, rem);
+        float w[V];
+        load_param<W, V>(g.w, c, rem, 1.f, w);
+#pragma unroll
+        for (int j = 0; j < V; j++) {
+            const float t = E::get(dy, j) * w[j];
+            s1 = fmaf(t, (E::get(x, j) - mean) * rstd, s1);
+            s2 += t;
+        }
+    }
+    s1 = lanes_sum<64>(s1);
+    s2 = lanes_sum<64>(s2);
+    if ((threadIdx.x & 63u) == 0) {
+        s_part[0][threadIdx.x >> 6] = s1;
+        s_part[1][threadIdx.x >> 6] = s2;
+    }
+    __syncthreads();
+    s1 = s2 = 0.f;
+#pragma unroll
+    for (int q = 0; q < 16; q++) {
+        s1 += s_part[0][q];
+        s2 += s_part[1][q];
+    }
+    s1 /= (float)g.cols;
+    s2 /= (float)g.cols;
+    uint8_t* dst = g.dx + row * g.lddx;
+    for (uint32_t c = threadIdx.x * V; c < g.cols; c += 1024 * V) {
+        const uint32_t rem = g.cols - c;
+        const u32x4 x = load_vec<E>(px, c, rem), dy = load_vec<E>(pdy, c, rem);
+        float w[V], o[V];
+        load_param<W, V>(g.w, c, rem, 1.f, w);
+#pragma unroll
+        for (int j = 0; j < V; j++)
+            o[j] = fmaf(-((E::get(x, j) - mean) * rstd), s1, fmaf(E::get(dy, j), w[j], -s2)) * rstd;
+        store_vec<E>(dst, c, rem, o);
+    }
+}
+
+// Sums of dy h and dy over a strip of rows (grid y), a vector of columns per
+// thread: the long rows' form of k_layer_norm_back's second result.
+template <class E>
+__global__ void __launch_bounds__(64) k_layer_norm_columns(LnBackArgs g) {
+    constexpr int V = E::vec;
+    const uint32_t c = (blockIdx.x * 64 + threadIdx.x) * V;
+    if (c >= g.cols) return;
+    const uint32_t rem = g.cols - c;
+    float dw[V], db[V];
+#pragma unroll
+    for (int j = 0; j < V; j++) dw[j] = db[j] = 0.f;
+    for (uint64_t row = blockIdx.y; row < g.rows; row += gridDim.y) {
+        const u32x4 x = load_vec<E>(g.x + row * g.ldx, c, rem), dy = load_vec<E>(g.dy + row * g.lddy, c, rem);
+        const float mean = g.mean[row], rstd = g.rstd[row];
+#pragma unroll
+        for (int j = 0; j < V; j++) {
+            const float d = E::get(dy, j);
+            dw[j] = fmaf(d, (E::get(x, j) - mean) * rstd, dw[j]);
+            db[j] += d;
+        }
+    }
+    float* part = g.part + (uint64_t)blockIdx.y * 2 * g.cols + c;
+#pragma unroll
+    for (int j = 0; j < V; j++)
+        if ((uint32_t)j < rem) {
+            part[j] = dw[j];
+            part[g.cols + j] = db[j];
+        }
+}
+
+// The weight's and the bias's gradient: the sums of `parts` blocks, in their
+// order (16 waves take every 16th each, then one adds the 16), onto what is
+// there where they accumulate.
+template <class G>
+__global__ void __launch_bounds__(1024) k_layer_norm_grads(const float* part, uint32_t parts, uint32_t cols,
+                                                           typename G::raw* dw, typename G::raw* db, int accumulate) {
+    __shared__ float s_sum[16][64];
+    const uint32_t wave = threadIdx.x >> 6, l = threadIdx.x & 63u;
+    const uint64_t c = (uint64_t)blockIdx.x * 64 + l;             // column of [dw | db]
+    const uint64_t width = 2ull * cols;
+    float sum = 0.f;
+    if (c < width)
+        for (uint32_t p = wave; p < parts; p += 16) sum += part[p * width + c];
+    s_sum[wave][l] = sum;
+    __syncthreads();
+    if (wave || c >= width) return;
+    float t = 0.f;
+#pragma unroll
+    for (int q = 0; q < 16; q++) t += s_sum[q][l];
+    typename G::raw* out = c < cols ? dw : db;
+    if (!out) return;
+    const uint64_t at = c < cols ? c : c - cols;
+    if (accumulate) t += G::one(out[at]);
+    out[at] = G::round(t);
+}
+
+// ---------------------------------------------------------------------------
+// host side
+
+inline bool dtype_ok(int32_t dt) { return dt == kF32 || dt == kBF16; }
+inline bool aligned(const void* p, int32_t dt) { return (reinterpret_cast<uintptr_t>(p) & (elem_bytes(dt) - 1)) == 0; }
+inline spccl_status_t launch_status() { return hipGetLastError() == hipSuccess ? SPCCL_OK : SPCCL_ERR_HIP; }
+
+// Whether two matrices of `rows` x `cols` elements share one.  Rows of the
+// same pitch may interleave (column ranges of one buffer).
+struct Rows {
+    const void* p;
+    uint64_t ld;              // elements between rows
+};
+bool rows_overlap(const Rows& a, const Rows& b, uint64_t rows, uint64_t cols, uint64_t s) {
+    if (!rows || !cols) return false;
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
+    const uint64_t an = ((rows - 1) * a.ld + cols) * s, bn = ((rows - 1) * b.ld + cols) * s;
+    if (x + an <= y || y + bn <= x) return false;
+    if (a.ld != b.ld) return true;
+    const uint64_t pitch = a.ld * s;
+    const uint64_t d = y >= x ? (y - x) % pitch : (pitch - (x - y) % pitch) % pitch;
+    return d < cols * s || pitch - d < cols * s;
+}
+bool span_overlap(const void* p, uint64_t pn, const Rows& m, uint64_t rows, uint64_t cols, uint64_t s) {
+    if (!p || !m.p || !pn || !rows || !cols) return false;
+    const uintptr_t x = reinterpret_cast<uintptr_t>(p), y = reinterpret_cast<uintptr_t>(m.p);
+    return x < y + ((rows - 1) * m.ld + cols) * s && y < x + pn;
+}
+
+// The layout of a row: lanes of a wave, or waves, and vectors per lane; calls
+// fn with the three as constants.  A block of 16 waves has 128 registers for
+// each lane: enough for a forward row of 32 elements, not for the backward
+// pass's rows and sums.
+constexpr uint32_t kMaxCols = 32768, kMaxBackCols = 16384;       // beyond: the long forms
+
+template <int N>
+using Int = std::integral_constant<int, N>;
+
+template <class E, bool Back, class Fn>
+auto with_row(uint32_t cols, Fn fn) {
+    constexpr int K1 = 8 / E::vec, K4 = 32 / E::vec;              // 8 and 32 elements per lane
+    if (cols <= 8 * 8) return fn(Int<8>{}, Int<1>{}, Int<K1>{});
+    if (cols <= 16 * 8) return fn(Int<16>{}, Int<1>{}, Int<K1>{});
+    if (cols <= 32 * 8) return fn(Int<32>{}, Int<1>{}, Int<K1>{});
+    if (cols <= 64 * 8) return fn(Int<64>{}, Int<1>{}, Int<K1>{});
+    if (cols <= 64 * 32) return fn(Int<64>{}, Int<1>{}, Int<K4>{});
+    if (cols <= 64 * 32 * 2) return fn(Int<64>{}, Int<2>{}, Int<K4>{});
+    if (cols <= 64 * 32 * 4) return fn(Int<64>{}, Int<4>{}, Int<K4>{});
+    if (Back || cols <= 64 * 32 * 8) return fn(Int<64>{}, Int<8>{}, Int<K4>{});
+    if constexpr (!Back) return fn(Int<64>{}, Int<16>{}, Int<K4>{});
+}
+
+template <class E, class W>
+spccl_status_t launch_forward(const LnArgs& g, hipStream_t st) {
+    if (g.cols > kMaxCols) {
+        hipLaunchKernelGGL((k_layer_norm_long<E, W>), dim3((uint32_t)g.rows), dim3(1024), 0, st, g);
+        return launch_status();
+    }
+    with_row<E, false>(g.cols, [&](auto l, auto waves, auto k) {
+        using R = Row<E, l(), waves(), k()>;
+        hipLaunchKernelGGL((k_layer_norm<E, W, l(), waves(), k()>), dim3((uint32_t)((g.rows + R::rows - 1) / R::rows)),
+                           dim3(R::threads), 0, st, g);
+    });
+    return launch_status();
+}
+
+// Blocks of a backward pass, each of which leaves two sums per column.
+constexpr uint32_t kBackBlocks = 1024, kStrips = 64;
+uint32_t back_blocks(uint64_t rows, uint32_t rows_per_block) {
+    const uint64_t b = (rows + rows_per_block - 1) / rows_per_block;
+    return (uint32_t)(b < kBackBlocks ? b : kBackBlocks);
+}
+uint32_t strips(uint64_t rows) { return (uint32_t)(rows < kStrips ? rows : kStrips); }
+
+template <class E>
+uint32_t back_parts(uint64_t rows, uint32_t cols) {
+    if (cols > kMaxBackCols) return strips(rows);
+    return with_row<E, true>(cols, [&](auto l, auto waves, auto k) {
+        return back_blocks(rows, Row<E, l(), waves(), k()>::rows);
+    });
+}
+
+template <class E, class W>
+spccl_status_t launch_backward(const LnBackArgs& g, int32_t gdtype, void* dw, void* db, int32_t accumulate,
+                               hipStream_t st) {
+    if (g.cols > kMaxBackCols) {
+        // the columns' sums first: dx may be written over dy or x
+        if (g.part) {
+            hipLaunchKernelGGL(k_layer_norm_columns<E>, dim3((g.cols + 64 * E::vec - 1) / (64 * E::vec), strips(g.rows)),
+                               dim3(64), 0, st, g);
+            if (launch_status() != SPCCL_OK) return SPCCL_ERR_HIP;
+        }
+        if (g.dx) hipLaunchKernelGGL((k_layer_norm_back_long<E, W>), dim3((uint32_t)g.rows), dim3(1024), 0, st, g);
+    } else {
+        with_row<E, true>(g.cols, [&](auto l, auto waves, auto k) {
+            using R = Row<E, l(), waves(), k()>;
+            hipLaunchKernelGGL((k_layer_norm_back<E, W, l(), waves(), k()>), dim3(back_blocks(g.rows, R::rows)),
+                               dim3(R::threads), 0, st, g);
+        });
+    }
+    if (launch_status() != SPCCL_OK) return SPCCL_ERR_HIP;
+    if (!g.part) return SPCCL_OK;
+    const uint32_t parts = back_parts<E>(g.rows, g.cols);
+    const dim3 grid((uint32_t)((2ull * g.cols + 63) / 64)), block(1024);
+    if (gdtype == kBF16)
+        hipLaunchKernelGGL(k_layer_norm_grads<BF16>, grid, block, 0, st, g.part, parts, g.cols,
+                           static_cast<uint16_t*>(dw), static_cast<uint16_t*>(db), accumulate);
+    else
+        hipLaunchKernelGGL(k_layer_norm_grads<F32>, grid, block, 0, st, g.part, parts, g.cols,
+                           static_cast<uint32_t*>(dw), static_cast<uint32_t*>(db), accumulate);
+    return launch_status();
+}
+
+}  // namespace
+}  // namespace spccl
+
+using namespace spccl;
+
+extern "C" {
+
+spccl_status_t spccl_layer_norm(const void* x, uint64_t ldx, const void* weight, const void* bias, void* y, uint64_t ldy,
+                                float* mean, float* rstd, uint64_t rows, uint64_t cols, int32_t dtype, int32_t wdtype,
+                                double eps, void* stream) {
+    if (!dtype_ok(dtype) || !dtype_ok(wdtype)) return SPCCL_ERR_UNSUPPORTED;
+    if (rows >= (1ull << 31) || cols >= (1ull << 31)) return SPCCL_ERR_UNSUPPORTED;
+    if (cols == 0 || ldx < cols || ldy < cols || !(eps >= 0.0)) return SPCCL_ERR_INVALID_ARG;
+    if (rows == 0) return SPCCL_OK;
+    if (!x || !y || !aligned(x, dtype) || !aligned(y, dtype) || !aligned(weight, wdtype) || !aligned(bias, wdtype) ||
+        !aligned(mean, kF32) || !aligned(rstd, kF32))
+        return SPCCL_ERR_INVALID_ARG;
+    const uint64_t s = elem_bytes(dtype), ws = elem_bytes(wdtype);
+    const Rows rx{x, ldx}, ry{y, ldy};
+    if (!(x == y && ldx == ldy) && rows_overlap(rx, ry, rows, cols, s)) return SPCCL_ERR_INVALID_ARG;
+    for (const Rows& m : {rx, ry})
+        if (span_overlap(mean, 4 * rows, m, rows, cols, s) || span_overlap(rstd, 4 * rows, m, rows, cols, s))
+            return SPCCL_ERR_INVALID_ARG;
+    if (span_overlap(weight, ws * cols, ry, rows, cols, s) || span_overlap(bias, ws * cols, ry, rows, cols, s))
+        return SPCCL_ERR_INVALID_ARG;
+    const LnArgs g{static_cast<const uint8_t*>(x), static_cast<const uint8_t*>(weight), static_cast<const uint8_t*>(bias),
+                   static_cast<uint8_t*>(y), mean, rstd, ldx * s, ldy * s, rows, (uint32_t)cols, (float)eps};
+    const hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+    if (dtype == kF32) return wdtype == kF32 ? launch_forward<F32, F32>(g, st) : launch_forward<F32, BF16>(g, st);
+    return wdtype == kF32 ? launch_forward<BF16, F32>(g, st) : launch_forward<BF16, BF16>(g, st);
+}
+
+uint64_t spccl_layer_norm_scratch_bytes(uint64_t rows, uint64_t cols) {
+    if (rows == 0 || rows >= (1ull << 31) || cols == 0 || cols >= (1ull << 31)) return 0;
+    // an fp32 row and a bf16 row of as many columns lie alike over the lanes
+    return 8ull * cols * back_parts<F32>(rows, (uint32_t)cols);
+}
+
+spccl_status_t spccl_layer_norm_backward(const void* dy, uint64_t lddy, const void* x, uint64_t ldx, const void* weight,
+                                         const float* mean, const float* rstd, void* dx, uint64_t lddx, void* dweight,
+                                         void* dbias, uint64_t rows, uint64_t cols, int32_t dtype, int32_t wdtype,
+                                         int32_t gdtype, int32_t accumulate, void* scratch, uint64_t scratch_bytes,
+                                         void* stream) {
+    if (!dtype_ok(dtype) || !dtype_ok(wdtype) || !dtype_ok(gdtype)) return SPCCL_ERR_UNSUPPORTED;
+    if (rows >= (1ull << 31) || cols >= (1ull << 31)) return SPCCL_ERR_UNSUPPORTED;
+    if (cols == 0 || lddy < cols || ldx < cols || (dx && lddx < cols)) return SPCCL_ERR_INVALID_ARG;
+    if (!aligned(dweight, gdtype) || !aligned(dbias, gdtype)) return SPCCL_ERR_INVALID_ARG;
+    const bool grads = dweight || dbias;
+    if (rows && (!dy || !x || !mean || !rstd || !aligned(dy, dtype) || !aligned(x, dtype) || !aligned(dx, dtype) ||
+                 !aligned(weight, wdtype) || !aligned(mean, kF32) || !aligned(rstd, kF32)))
+        return SPCCL_ERR_INVALID_ARG;
+    const uint64_t s = elem_bytes(dtype), gs = elem_bytes(gdtype);
+    const uint64_t need = grads ? spccl_layer_norm_scratch_bytes(rows, cols) : 0;
+    if (need) {
+        if (!scratch || (reinterpret_cast<uintptr_t>(scratch) & 15u)) return SPCCL_ERR_INVALID_ARG;
+        if (scratch_bytes < need) return SPCCL_ERR_WORKSPACE;
+    }
+    const Rows rdy{dy, lddy}, rx{x, ldx}, rdx{dx, lddx};
+    if (rows && dx) {
+        if (!(dx == dy && lddx == lddy) && rows_overlap(rdx, rdy, rows, cols, s)) return SPCCL_ERR_INVALID_ARG;
+        if (!(dx == x && lddx == ldx) && rows_overlap(rdx, rx, rows, cols, s)) return SPCCL_ERR_INVALID_ARG;
+        if (span_overlap(weight, elem_bytes(wdtype) * cols, rdx, rows, cols, s) ||
+            span_overlap(mean, 4 * rows, rdx, rows, cols, s) || span_overlap(rstd, 4 * rows, rdx, rows, cols, s))
+            return SPCCL_ERR_INVALID_ARG;
+    }
+    const Rows d[3] = {rdy, rx, rdx};
+    for (const Rows& m : d)
+        if (span_overlap(dweight, gs * cols, m, rows, cols, s) || span_overlap(dbias, gs * cols, m, rows, cols, s) ||
+            (need && span_overlap(scratch, need, m, rows, cols, s)))
+            return SPCCL_ERR_INVALID_ARG;
+    const Rows one[2] = {{dweight, cols}, {dbias, cols}};
+    if (span_overlap(dweight, gs * cols, one[1], 1, cols, gs)) return SPCCL_ERR_INVALID_ARG;
+    for (const Rows& m : one)
+        if (need && span_overlap(scratch, need, m, 1, cols, gs)) return SPCCL_ERR_INVALID_ARG;
+    const LnBackArgs g{static_cast<const uint8_t*>(dy), static_cast<const uint8_t*>(x), static_cast<const uint8_t*>(weight),
+                       mean, rstd, static_cast<uint8_t*>(dx), grads ? static_cast<float*>(scratch) : nullptr,
+                       lddy * s, ldx * s, lddx * s, rows, (uint32_t)cols};
+    const hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+    if (rows == 0) {
+        // no rows: the sums are zero
+        if (!grads || accumulate) return SPCCL_OK;
+        const dim3 grid((uint32_t)((2 * cols + 63) / 64)), block(1024);
+        if (gdtype == kBF16)
+            hipLaunchKernelGGL(k_layer_norm_grads<BF16>, grid, block, 0, st, static_cast<const float*>(nullptr), 0u,
+                               (uint32_t)cols, static_cast<uint16_t*>(dweight), static_cast<uint16_t*>(dbias), 0);
+        else
+            hipLaunchKernelGGL(k_layer_norm_grads<F32>, grid, block, 0, st, static_cast<const float*>(nullptr), 0u,
+                               (uint32_t)cols, static_cast<uint32_t*>(dweight), static_cast<uint32_t*>(dbias), 0);
+        return launch_status();
+    }
+    if (!dx && !grads) return SPCCL_OK;
+    if (dtype == kF32)
+        return wdtype == kF32 ? launch_backward<F32, F32>(g, gdtype, dweight, dbias, accumulate, st)
+                              : launch_backward<F32, BF16>(g, gdtype, dweight, dbias, accumulate, st);
+    return wdtype == kF32 ? launch_backward<BF16, F32>(g, gdtype, dweight, dbias, accumulate, st)
+                          : launch_backward<BF16, BF16>(g, gdtype, dweight, dbias, accumulate, st);
+}
+
+}  // extern "C"
