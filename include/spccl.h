@@ -504,6 +504,99 @@ spccl_status_t spccl_layer_norm_backward(const void* dy, uint64_t lddy, const vo
                                          int32_t gdtype, int32_t accumulate, void* scratch, uint64_t scratch_bytes,
                                          void* stream);
 
+/* ---- pruning with error feedback (Sec. VI-B) --------------------------------- */
+
+/* Splits a gradient and its residual by magnitude, for each of n elements
+ * (n < 2^40):
+ *   a = grad + leak * residual         (fp32, each operation rounded)
+ *   out = a rounded to dtype where |a| >= *threshold, +0.0 elsewhere
+ *   residual = a - out
+ * so what is not sent now is added to a later gradient (leak = 1; below 1 old
+ * residuals fade), and in bf16 the sent values' rounding errors as well.  The
+ * result is what the codec and the collectives take.  grad and out have
+ * `dtype`; out may be grad itself; residual is fp32.  threshold: a device
+ * value, e.g. a quantile of a sample of |a|.  A NaN, an infinity, or a value
+ * that overflows dtype is sent and leaves no residual; a NaN threshold sends
+ * everything; a zero is never sent as -0.0. */
+spccl_status_t spccl_prune(const void* grad, float* residual, const float* threshold, double leak, void* out, uint64_t n,
+                           int32_t dtype, void* stream);
+
+/* ---- AdamW over many tensors at once ------------------------------------------ */
+
+/* First and second moments in fp32, or in 8 bits: OCP E4M3 values times a
+ * power of two shared by a block of SPCCL_STATE_BLOCK consecutive elements of
+ * the tensor (one byte per block, the exponent biased by 127; the last block
+ * may be short).  A scale brings its block's largest magnitude into [2^7,
+ * 2^8).  8-bit moments are rounded stochastically; a second moment above zero
+ * stays at least the smallest value; a block that holds a NaN or an infinity
+ * has the scale 255 and stands for NaN.  All-zero bytes are zero moments. */
+typedef enum { SPCCL_STATE_F32 = 0, SPCCL_STATE_F8 = 1 } spccl_state_t;
+#define SPCCL_STATE_BLOCK 32
+
+/* One tensor (host struct of device pointers).  Every array holds n elements
+ * (n < 2^32) and is aligned to its element; tensors of a plan share param,
+ * gradient and state types. */
+typedef struct {
+    void* param;             /* fp32 or bf16; bf16 is rounded stochastically, as 16 bits
+                                would otherwise lose small updates */
+    void* model;             /* bf16 copy of an fp32 param, written with it (NULL: none) */
+    spccl_operand_t grad;    /* ARRAY of n elements, or STREAM: a PICI or DENSE message
+                                (the header says which) that holds the tensor's gradient
+                                among others, such as a whole bucket's */
+    uint64_t grad_offset;    /* STREAM: the tensor's first element in the message, a
+                                multiple of 64 */
+    uint64_t grad_n;         /* STREAM: elements of the message */
+    void* m;                 /* first moment: fp32, or one byte per element */
+    void* v;                 /* second moment */
+    void* m_scale;           /* 8-bit states: ceil(n / SPCCL_STATE_BLOCK) bytes; else NULL */
+    void* v_scale;
+    uint64_t n;
+    double weight_decay;     /* >= 0 */
+} spccl_adamw_tensor_t;
+
+/* What a step needs to know about its tensors (host struct, filled in by
+ * spccl_adamw_plan).  It stays valid while the tensors and the table stay
+ * where they are. */
+typedef struct {
+    uint32_t magic;
+    int32_t param_dtype, grad_dtype, state, count, pad;
+    uint64_t array_chunks, stream_chunks;
+    void* table;
+} spccl_adamw_plan_t;
+
+/* Lays a plan for `count` tensors (host array) out in `table` (device, 16-byte
+ * aligned, spccl_adamw_plan_bytes(tensors, count) bytes, which the plan uses
+ * until it is dropped), with small kernels on `stream`.  Refuses overlaps of
+ * anything a step writes with anything else (SPCCL_ERR_INVALID_ARG); gradients
+ * may be shared.  COO gradients: SPCCL_ERR_UNSUPPORTED. */
+uint64_t spccl_adamw_plan_bytes(const spccl_adamw_tensor_t* tensors, int32_t count);
+spccl_status_t spccl_adamw_plan(const spccl_adamw_tensor_t* tensors, int32_t count, int32_t param_dtype, int32_t grad_dtype,
+                                int32_t state, void* table, uint64_t table_bytes, spccl_adamw_plan_t* plan, void* stream);
+
+typedef struct {
+    double lr;               /* >= 0 */
+    double beta1, beta2;     /* in [0, 1) */
+    double eps;              /* >= 0 */
+    uint64_t step;           /* t >= 1, for the bias corrections */
+    uint64_t seed;           /* of the stochastic rounding: give each step another */
+} spccl_adamw_t;
+
+/* One step over a plan's tensors, one launch for those with ARRAY gradients
+ * and one for those with STREAM gradients:
+ *   g = grad * *grad_scale                  (device value; NULL: 1)
+ *   m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2
+ *   param = param (1 - lr weight_decay)
+ *           - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
+ * in fp32, each operation rounded, with m and v as they are before they are
+ * rounded to 8 bits.  An element that a message leaves out has a gradient of
+ * zero.  Element i of tensor k takes its random bits from the seed and from
+ * i + the sum over earlier tensors of n rounded up to 64: equal calls give
+ * equal bits.  ws: at least the 256-byte control block of a workspace; a
+ * message that fails its header checks sets SPCCL_ERR_CORRUPT_STREAM there and
+ * its tensors are not changed; a tile that fails its checks counts as empty. */
+spccl_status_t spccl_adamw_step(const spccl_adamw_plan_t* plan, const spccl_adamw_t* hyper, const float* grad_scale,
+                                void* ws, uint64_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -28,6 +28,8 @@ STATUS_NAMES = {0: "OK", 1: "ERR_INVALID_ARG", 2: "ERR_CAPACITY", 3: "ERR_UNSUPP
 SPCCL_F32, SPCCL_BF16 = 0, 1
 SPCCL_FMT_DENSE, SPCCL_FMT_PICI, SPCCL_FMT_COO = 0, 1, 2
 SPCCL_ARRAY, SPCCL_STREAM = 0, 1
+SPCCL_STATE_F32, SPCCL_STATE_F8 = 0, 1
+SPCCL_STATE_BLOCK = 32
 HEADER_BYTES = 48
 NNZ_UNKNOWN = (1 << 64) - 1
 
@@ -44,7 +46,8 @@ EXPORTS = ("spccl_num_tiles", "spccl_pici_bytes", "spccl_stream_bound", "spccl_w
            "spccl_reduce_sliced_tracked", "spccl_vr_sliced_scratch_bytes", "spccl_vr_reduce_scatter_sliced",
            "spccl_vr_all_gather_sliced", "spccl_vr_all_reduce_sliced", "spccl_compress_static",
            "spccl_set_single_pass_limit", "spccl_layer_norm", "spccl_layer_norm_scratch_bytes",
-           "spccl_layer_norm_backward")
+           "spccl_layer_norm_backward", "spccl_prune", "spccl_adamw_plan_bytes", "spccl_adamw_plan",
+           "spccl_adamw_step")
 
 
 class spccl_operand_t(ctypes.Structure):
@@ -68,6 +71,24 @@ class spccl_trace_t(ctypes.Structure):
     _fields_ = [("step", ctypes.c_int32), ("rank", ctypes.c_int32), ("fmt", ctypes.c_int32),
                 ("measured", ctypes.c_int32), ("bytes", ctypes.c_uint64), ("nnz", ctypes.c_uint64),
                 ("sigma", ctypes.c_double)]
+
+
+class spccl_adamw_tensor_t(ctypes.Structure):
+    _fields_ = [("param", ctypes.c_void_p), ("model", ctypes.c_void_p), ("grad", spccl_operand_t),
+                ("grad_offset", ctypes.c_uint64), ("grad_n", ctypes.c_uint64), ("m", ctypes.c_void_p),
+                ("v", ctypes.c_void_p), ("m_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+                ("n", ctypes.c_uint64), ("weight_decay", ctypes.c_double)]
+
+
+class spccl_adamw_plan_t(ctypes.Structure):
+    _fields_ = [("magic", ctypes.c_uint32), ("param_dtype", ctypes.c_int32), ("grad_dtype", ctypes.c_int32),
+                ("state", ctypes.c_int32), ("count", ctypes.c_int32), ("pad", ctypes.c_int32),
+                ("array_chunks", ctypes.c_uint64), ("stream_chunks", ctypes.c_uint64), ("table", ctypes.c_void_p)]
+
+
+class spccl_adamw_t(ctypes.Structure):
+    _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double),
+                ("eps", ctypes.c_double), ("step", ctypes.c_uint64), ("seed", ctypes.c_uint64)]
 
 
 _u64, _i32, _vp = ctypes.c_uint64, ctypes.c_int32, ctypes.c_void_p
@@ -124,6 +145,11 @@ _sigs = {
     "spccl_layer_norm_scratch_bytes": (_u64, [_u64, _u64]),
     "spccl_layer_norm_backward": (_i32, [_vp, _u64, _vp, _u64, _vp, _vp, _vp, _vp, _u64, _vp, _vp, _u64, _u64, _i32, _i32,
                                          _i32, _i32, _vp, _u64, _vp]),
+    "spccl_prune": (_i32, [_vp, _vp, _vp, ctypes.c_double, _vp, _u64, _i32, _vp]),
+    "spccl_adamw_plan_bytes": (_u64, [ctypes.POINTER(spccl_adamw_tensor_t), _i32]),
+    "spccl_adamw_plan": (_i32, [ctypes.POINTER(spccl_adamw_tensor_t), _i32, _i32, _i32, _i32, _vp, _u64,
+                                ctypes.POINTER(spccl_adamw_plan_t), _vp]),
+    "spccl_adamw_step": (_i32, [ctypes.POINTER(spccl_adamw_plan_t), ctypes.POINTER(spccl_adamw_t), _vp, _vp, _u64, _vp]),
 }
 for _name, (_res, _args) in _sigs.items():
     _f = getattr(_lib, _name)
@@ -503,6 +529,106 @@ def spccl_layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: torch.T
         _dt(x) if weight is None else _dt(weight), _dt_of_pair(dweight, dbias, SPCCL_F32, "dweight and dbias"),
         1 if accumulate else 0, _ptr_or_null(scratch), 0 if scratch is None else _nbytes(scratch), _stream(stream)),
         "spccl_layer_norm_backward")
+
+
+# ---- pruning and AdamW ---------------------------------------------------------------
+
+def spccl_prune(grad: torch.Tensor, residual: torch.Tensor, threshold: torch.Tensor, leak: float, out: torch.Tensor,
+                stream=None) -> None:
+    """Split grad + leak * residual: what reaches the threshold (a device value)
+    goes to out (which may be grad), the rest stays in residual (fp32)."""
+    n = grad.numel()
+    if not (grad.is_contiguous() and residual.is_contiguous() and out.is_contiguous()):
+        raise ValueError("spccl_prune: contiguous tensors are needed")
+    if residual.numel() != n or out.numel() != n or out.dtype != grad.dtype or residual.dtype != torch.float32 \
+            or threshold.numel() != 1 or threshold.dtype != torch.float32:
+        raise ValueError("spccl_prune: residual (fp32) and out (grad's dtype) hold grad's elements, threshold one fp32")
+    _check(_lib.spccl_prune(grad.data_ptr(), residual.data_ptr(), threshold.data_ptr(), float(leak), out.data_ptr(), n,
+                            _dt(grad), _stream(stream)), "spccl_prune")
+
+
+def adamw_tensor(param: torch.Tensor, grad, m: torch.Tensor, v: torch.Tensor, m_scale: torch.Tensor | None = None,
+                 v_scale: torch.Tensor | None = None, model: torch.Tensor | None = None, weight_decay: float = 0.0,
+                 grad_dtype: int | None = None, grad_offset: int = 0, grad_n: int = 0) -> spccl_adamw_tensor_t:
+    """One tensor of an AdamW plan.  grad is a tensor of param's elements, or an
+    operand: then grad_dtype (SPCCL_F32 or SPCCL_BF16) and, for a message, the
+    tensor's place grad_offset among its grad_n elements are given too.  m and v
+    are fp32, or one byte per element (float8_e4m3fn or uint8) with m_scale and
+    v_scale (float8_e8m0fnu or uint8), one per SPCCL_STATE_BLOCK elements.  It
+    holds references to its tensors."""
+    n = param.numel()
+    eight = m.dtype != torch.float32
+    tensors = [("param", param, n, None), ("m", m, n, None), ("v", v, n, m.dtype)]
+    if model is not None:
+        tensors.append(("model", model, n, torch.bfloat16))
+    if isinstance(grad, torch.Tensor):
+        tensors.append(("grad", grad, n, None))
+    if eight:
+        if m.element_size() != 1 or m_scale is None or v_scale is None:
+            raise ValueError("adamw_tensor: 8-bit moments take one byte per element and their scales")
+        blocks = -(-n // SPCCL_STATE_BLOCK)
+        tensors += [("m_scale", m_scale, blocks, None), ("v_scale", v_scale, blocks, m_scale.dtype)]
+        if m_scale.element_size() != 1:
+            raise ValueError("adamw_tensor: a scale is one byte")
+    elif m_scale is not None or v_scale is not None:
+        raise ValueError("adamw_tensor: fp32 moments have no scales")
+    for what, t, size, dt in tensors:
+        if t.numel() != size or not t.is_contiguous() or (dt is not None and t.dtype != dt):
+            raise ValueError(f"adamw_tensor: {what} needs {size} contiguous elements{f' of {dt}' if dt else ''}, got "
+                             f"{tuple(t.shape)} {t.dtype}")
+    if isinstance(grad, torch.Tensor):
+        op, gdt = operand(grad), _dt(grad)
+    elif grad_dtype is None:
+        raise ValueError("adamw_tensor: an operand's grad_dtype is needed")
+    else:
+        op, gdt = grad, grad_dtype
+    t = spccl_adamw_tensor_t(param.data_ptr(), _ptr_or_null(model), op, grad_offset, grad_n, m.data_ptr(), v.data_ptr(),
+                             _ptr_or_null(m_scale), _ptr_or_null(v_scale), n, weight_decay)
+    t._types = (_dt(param), gdt, SPCCL_STATE_F8 if eight else SPCCL_STATE_F32)
+    t._tensors = (param, grad, m, v, m_scale, v_scale, model)
+    return t
+
+
+def alloc_adamw_state(n: int, state: int = SPCCL_STATE_F32, device="cuda") -> dict:
+    """Zeroed moments of n elements, as adamw_tensor's keywords m, v (and m_scale, v_scale)."""
+    if state == SPCCL_STATE_F32:
+        return {k: torch.zeros(n, dtype=torch.float32, device=device) for k in ("m", "v")}
+    blocks = -(-n // SPCCL_STATE_BLOCK)
+    out = {k: torch.zeros(n, dtype=torch.uint8, device=device).view(torch.float8_e4m3fn) for k in ("m", "v")}
+    for k in ("m_scale", "v_scale"):
+        out[k] = torch.zeros(blocks, dtype=torch.uint8, device=device).view(torch.float8_e8m0fnu)
+    return out
+
+
+def spccl_adamw_plan_bytes(tensors: list) -> int:
+    return _lib.spccl_adamw_plan_bytes((spccl_adamw_tensor_t * len(tensors))(*tensors), len(tensors))
+
+
+def spccl_adamw_plan(tensors: list, table: torch.Tensor, stream=None) -> spccl_adamw_plan_t:
+    """A plan over tensors made by adamw_tensor, laid out in table (bytes on the
+    device).  It holds references to both."""
+    kinds = {t._types for t in tensors}
+    if len(kinds) > 1:
+        raise ValueError(f"spccl_adamw_plan: (param, gradient, state) types differ: {sorted(kinds)}")
+    pdt, gdt, state = kinds.pop() if kinds else (SPCCL_F32, SPCCL_F32, SPCCL_STATE_F32)
+    plan = spccl_adamw_plan_t()
+    _check(_lib.spccl_adamw_plan((spccl_adamw_tensor_t * len(tensors))(*tensors), len(tensors), pdt, gdt, state,
+                                 table.data_ptr(), _nbytes(table), ctypes.byref(plan), _stream(stream)),
+           "spccl_adamw_plan")
+    plan._tensors = (list(tensors), table)
+    return plan
+
+
+def spccl_adamw_step(plan: spccl_adamw_plan_t, ws: torch.Tensor, lr: float, beta1: float = 0.9, beta2: float = 0.999,
+                     eps: float = 1e-8, step: int = 1, seed: int = 0, grad_scale: torch.Tensor | None = None,
+                     stream=None) -> None:
+    """One AdamW step over the plan's tensors; gradients are multiplied by
+    grad_scale (one fp32 on the device) first."""
+    if grad_scale is not None and (grad_scale.numel() != 1 or grad_scale.dtype != torch.float32):
+        raise ValueError("spccl_adamw_step: grad_scale is one fp32")
+    h = spccl_adamw_t(lr, beta1, beta2, eps, step, seed)
+    _check(_lib.spccl_adamw_step(ctypes.byref(plan), ctypes.byref(h), _ptr_or_null(grad_scale), ws.data_ptr(),
+                                 _nbytes(ws), _stream(stream)), "spccl_adamw_step")
 
 
 # ---- tensor helpers (allocation stays with the caller; these only size buffers) -----

@@ -1,0 +1,156 @@
+"""Pruning with error feedback.  Its sums are defined as held in fp32 (each
+operation rounded), so the expected values, computed in 64 bits and rounded
+where the definition rounds, are exact: no tolerance."""
+import numpy as np
+import pytest
+
+from helpers import log
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+@pytest.fixture(scope="module")
+def S():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    import paper_2607_04676_amd as S
+    return S
+
+
+def expected(grad, residual, tau, leak, dtype):
+    leak = np.float64(np.float32(leak))
+    with np.errstate(over="ignore", invalid="ignore"):
+        carried = (residual.astype(np.float64) * leak).astype(np.float32).astype(np.float64)
+        a = (grad.astype(np.float64) + carried).astype(np.float32)
+        sent = np.where((np.abs(a) < tau) | (a == 0), np.float32(0), a)
+        if dtype == "bf16":
+            sent = torch.from_numpy(sent).to(torch.bfloat16).float().numpy()
+        back = np.where(np.isfinite(sent), (a.astype(np.float64) - sent).astype(np.float32), np.float32(0))
+    return sent, back
+
+
+def same(got, exp):
+    """Equal bits, but any NaN for a NaN."""
+    both = np.isnan(got) & np.isnan(exp)
+    return np.array_equal(np.where(both, 0, got.view(np.uint32)), np.where(both, 0, exp.view(np.uint32)))
+
+
+def inputs(n, dtype, seed, offset=0):
+    rng = np.random.default_rng(seed)
+    grad = torch.from_numpy(rng.normal(0, 1e-3, n + offset).astype(np.float32)).to(DT[dtype])
+    residual = torch.from_numpy(rng.normal(0, 5e-4, n + offset).astype(np.float32))
+    return grad, residual
+
+
+@pytest.mark.parametrize("n", [1, 2, 3, 4, 5, 63, 255, 1024, 4095, 4096, 4097, 10_007, 1 << 20, (1 << 22) + 3])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("leak,offset", [(1.0, 0), (0.9, 1), (0.0, 3)])
+def test_split(S, n, dtype, leak, offset):
+    log(f"prune n={n} {dtype} leak={leak}")
+    grad, residual = inputs(n, dtype, n, offset)
+    tau = np.float32(1.5e-3)
+    g, r = grad.cuda()[offset:], residual.cuda()[offset:]
+    out = torch.full((n + 8,), 7.0, dtype=DT[dtype], device="cuda")
+    before = r.clone()
+    S.spccl_prune(g, r, torch.tensor([tau], device="cuda"), leak, out[:n])
+    torch.cuda.synchronize()
+    sent, back = expected(grad[offset:].float().numpy(), residual[offset:].numpy(), tau, leak, dtype)
+    assert same(out[:n].float().cpu().numpy(), sent)
+    assert same(r.cpu().numpy(), back)
+    assert torch.equal(out[n:], torch.full((8,), 7.0, dtype=DT[dtype], device="cuda"))
+    # over the gradient itself
+    r2, g2 = before.clone(), g.clone()
+    S.spccl_prune(g2, r2, torch.tensor([tau], device="cuda"), leak, g2)
+    torch.cuda.synchronize()
+    assert torch.equal(g2, out[:n]) and torch.equal(r2, r)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_special_values(S, dtype):
+    """Zeros of either sign are absent; what is not finite, or overflows, is
+    sent and leaves no residual; thresholds of 0, infinity and NaN."""
+    log(f"prune special {dtype}")
+    big = 3.4e38
+    grad = np.array([0.0, -0.0, np.nan, np.inf, -np.inf, big, -big, 1e-40, -1e-40, 1.0, 1e-3, -1.0, 0.0], np.float32)
+    res = np.array([0.0, -0.0, 1.0, 1.0, np.inf, big, 1.0, 0.0, 1e-41, 1e-8, np.nan, 1.0, -np.inf], np.float32)
+    t = torch.from_numpy(grad).to(DT[dtype])
+    for tau in (0.0, 1e-3, np.inf, np.nan):
+        g, r = t.cuda(), torch.from_numpy(res).cuda()
+        out = torch.empty_like(g)
+        S.spccl_prune(g, r, torch.tensor([tau], device="cuda"), 1.0, out)
+        torch.cuda.synchronize()
+        sent, back = expected(t.float().numpy(), res, np.float32(tau), 1.0, dtype)
+        assert same(out.float().cpu().numpy(), sent), tau
+        assert same(r.cpu().numpy(), back), tau
+        assert np.isfinite(r.cpu().numpy()).all()
+        bits = out.view(torch.int32 if dtype == "f32" else torch.int16).cpu().numpy()
+        assert bits[0] == 0 and bits[1] == 0
+
+
+def test_nothing_is_lost(S):
+    """Over rounds with leak 1, what was sent plus what stays is what came in."""
+    log("prune conservation")
+    n, rounds = 30_000, 6
+    rng = np.random.default_rng(3)
+    # multiples of 2^-12 below 2^2: every sum of six of them is exact in fp32
+    grads = rng.integers(-8000, 8000, (rounds, n)).astype(np.float64) / 4096
+    r = torch.zeros(n, device="cuda")
+    out = torch.empty(n, device="cuda")
+    sent = np.zeros(n)
+    for k in range(rounds):
+        S.spccl_prune(torch.from_numpy(grads[k].astype(np.float32)).cuda(), r, torch.tensor([1.9], device="cuda"), 1.0, out)
+        sent += out.double().cpu().numpy()
+    assert np.array_equal(sent + r.double().cpu().numpy(), grads.sum(0))
+    assert 0 < np.count_nonzero(out.cpu().numpy()) < n
+
+
+def test_past_32_bit_offsets(S):
+    log("prune large")
+    n = (1 << 32) + 4099
+    g = torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+    r = torch.zeros(n, device="cuda")
+    at = [0, (1 << 30) + 1, (1 << 31) - 1, 1 << 31, (1 << 32) - 1, 1 << 32, n - 1]
+    for k, i in enumerate(at):
+        g[i] = k + 1
+        r[i] = 0.25
+    S.spccl_prune(g, r, torch.tensor([3.0], device="cuda"), 1.0, g)
+    torch.cuda.synchronize()
+    assert int(torch.count_nonzero(g.view(torch.int16))) == len(at) - 2
+    for k, i in enumerate(at):
+        assert float(g[i]) == (k + 1.25 if k >= 2 else 0.0)
+        assert float(r[i]) == (0.0 if k >= 2 else k + 1.25)
+
+
+def test_message_of_a_pruned_gradient(S):
+    """The result is what the codec takes: its message holds the sent values."""
+    log("prune and compress")
+    n = 100_003
+    grad, residual = inputs(n, "f32", 9)
+    tau = np.float32(2.5e-3)
+    out = torch.empty(n, device="cuda")
+    S.spccl_prune(grad.cuda(), residual.cuda(), torch.tensor([tau], device="cuda"), 1.0, out)
+    ws, msg = S.alloc_workspace(n, S.SPCCL_F32), S.alloc_stream(n, S.SPCCL_F32)
+    S.spccl_compress(out, msg, ws)
+    back = torch.empty(n, device="cuda")
+    S.spccl_decompress(msg, back, ws)
+    torch.cuda.synchronize()
+    sent, _ = expected(grad.numpy(), residual.numpy(), tau, 1.0, "f32")
+    assert S.spccl_read_status(ws) == 0
+    assert S.spccl_read_header(msg)["nnz"] == np.count_nonzero(sent)
+    assert same(back.cpu().numpy(), sent)
+
+
+def test_binding_refuses(S):
+    x = torch.zeros(8, device="cuda")
+    tau = torch.zeros(1, device="cuda")
+    for f in (lambda: S.spccl_prune(x, x[:7].clone(), tau, 1.0, x), lambda: S.spccl_prune(x, x.clone(), x, 1.0, x),
+              lambda: S.spccl_prune(x, x.bfloat16(), tau, 1.0, x), lambda: S.spccl_prune(x[::2], x[:4], tau, 1.0, x[:4]),
+              lambda: S.spccl_prune(x, x.clone(), tau, 1.0, x.bfloat16())):
+        with pytest.raises(ValueError):
+            f()
+    with pytest.raises(S.SpcclError):
+        S.spccl_prune(x, x, tau, 1.0, x)
