@@ -7,9 +7,8 @@
 //   AdamW   m = b1 m + (1 - b1) g,  v = b2 v + (1 - b2) g^2,
 //           p = p (1 - lr wd) - lr / (1 - b1^t) m / (sqrt(v) / sqrt(1 - b2^t) + eps)
 //
-// Both are bound by memory: every array is read and written once, with
-// 16 bytes in flight per lane and array, and nothing is kept for a second
-// pass.  All arithmetic is fp32, each operation rounded by itself (no
+// Both are bound by memory: every array is read and written once and nothing is
+// kept for a second pass.  All arithmetic is fp32, each operation rounded by itself (no
 // contraction), so equal inputs give equal bits wherever it is computed.
 #include <hip/hip_runtime.h>
 #include <math.h>
@@ -37,63 +36,90 @@ __device__ __forceinline__ uint32_t bf16_pair(float a, float b) {         // nea
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, bf16x2));
 }
 
-// Four consecutive elements of a dtype, `rem` of which exist (the others read
-// 0 and are not written).
+// A place in global memory, as a base that the whole block shares (scalar
+// registers) and a lane's offset in bytes.  A table's addresses are numbers to
+// the compiler; without the address space it would take generic accesses, which
+// count against the LDS as well and kept an 8-bit step of 10^8 elements at 485
+// us instead of 299.
+template <class T>
+__device__ __forceinline__ T __attribute__((address_space(1))) * at(uint64_t base, uint32_t offset) {
+    return (T __attribute__((address_space(1)))*)(base + offset);
+}
+
+// Four consecutive elements from element o of a chunk on, `rem` of which exist
+// (Full: all; the others read 0 and are not written).  Every array is read
+// once and written once a call, so all accesses are non-temporal: an fp32 step
+// of 2^28 elements takes 1338 us so and 1455 through the caches, an 8-bit one
+// of 10^8 263 and 291 (at 2^22 elements, which the caches hold from call to
+// call, 20.7 and 19.2).
 struct Quad {
     float f[4];
 };
-
-template <int DT>
-__device__ __forceinline__ Quad load_quad(const uint8_t* base, uint64_t e, uint32_t rem) {
+template <int DT, bool Full>
+__device__ __forceinline__ Quad get4(uint64_t base, uint32_t o, uint32_t rem) {
     Quad q{{0.f, 0.f, 0.f, 0.f}};
     if constexpr (DT == kF32) {
-        const uint32_t* p = reinterpret_cast<const uint32_t*>(base) + e;
-        if (rem >= 4) {
-            const u32x4 v = *reinterpret_cast<const u32x4_any*>(p);
+        if (Full || rem >= 4) {
+            const u32x4 v = __builtin_nontemporal_load(at<const u32x4_any>(base, 4 * o));
 #pragma unroll
             for (int j = 0; j < 4; j++) q.f[j] = __uint_as_float(v[j]);
         } else {
 #pragma unroll
             for (int j = 0; j < 3; j++)
-                if ((uint32_t)j < rem) q.f[j] = __uint_as_float(p[j]);
+                if ((uint32_t)j < rem) q.f[j] = __uint_as_float(at<const uint32_t>(base, 4 * o)[j]);
         }
     } else {
-        const uint16_t* p = reinterpret_cast<const uint16_t*>(base) + e;
-        if (rem >= 4) {
-            const u32x2 v = *reinterpret_cast<const u32x2_any*>(p);
+        if (Full || rem >= 4) {
+            const u32x2 v = __builtin_nontemporal_load(at<const u32x2_any>(base, 2 * o));
 #pragma unroll
             for (int j = 0; j < 4; j++) q.f[j] = __uint_as_float(j & 1 ? v[j / 2] & 0xFFFF0000u : v[j / 2] << 16);
         } else {
 #pragma unroll
             for (int j = 0; j < 3; j++)
-                if ((uint32_t)j < rem) q.f[j] = __uint_as_float((uint32_t)p[j] << 16);
+                if ((uint32_t)j < rem) q.f[j] = __uint_as_float((uint32_t)at<const uint16_t>(base, 2 * o)[j] << 16);
         }
     }
     return q;
 }
-
-__device__ __forceinline__ void store_f32(uint8_t* base, uint64_t e, uint32_t rem, const float* f) {
-    uint32_t* p = reinterpret_cast<uint32_t*>(base) + e;
-    if (rem >= 4) {
-        *reinterpret_cast<u32x4_any*>(p) =
-            u32x4{__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])};
+template <bool Full>
+__device__ __forceinline__ void put4_f32(uint64_t base, uint32_t o, uint32_t rem, const float* f) {
+    if (Full || rem >= 4) {
+        const u32x4 v{__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])};
+        __builtin_nontemporal_store(v, at<u32x4_any>(base, 4 * o));
         return;
     }
 #pragma unroll
     for (int j = 0; j < 3; j++)
-        if ((uint32_t)j < rem) p[j] = __float_as_uint(f[j]);
+        if ((uint32_t)j < rem) at<uint32_t>(base, 4 * o)[j] = __float_as_uint(f[j]);
 }
-
-// two packed pairs of 16-bit elements
-__device__ __forceinline__ void store_16(uint8_t* base, uint64_t e, uint32_t rem, u32x2 v) {
-    uint16_t* p = reinterpret_cast<uint16_t*>(base) + e;
-    if (rem >= 4) {
-        *reinterpret_cast<u32x2_any*>(p) = v;
+template <bool Full>
+__device__ __forceinline__ void put4_16(uint64_t base, uint32_t o, uint32_t rem, u32x2 v) {
+    if (Full || rem >= 4) {
+        __builtin_nontemporal_store(v, at<u32x2_any>(base, 2 * o));
         return;
     }
 #pragma unroll
     for (int j = 0; j < 3; j++)
-        if ((uint32_t)j < rem) p[j] = (uint16_t)(v[j / 2] >> (16 * (j & 1)));
+        if ((uint32_t)j < rem) at<uint16_t>(base, 2 * o)[j] = (uint16_t)(v[j / 2] >> (16 * (j & 1)));
+}
+template <bool Full>
+__device__ __forceinline__ uint32_t get4_8(uint64_t base, uint32_t o, uint32_t rem) {
+    if (Full || rem >= 4) return __builtin_nontemporal_load(at<const u32_any>(base, o));
+    uint32_t w = 0;
+#pragma unroll
+    for (int j = 0; j < 3; j++)
+        if ((uint32_t)j < rem) w |= (uint32_t)at<const uint8_t>(base, o)[j] << (8 * j);
+    return w;
+}
+template <bool Full>
+__device__ __forceinline__ void put4_8(uint64_t base, uint32_t o, uint32_t rem, uint32_t w) {
+    if (Full || rem >= 4) {
+        __builtin_nontemporal_store(w, at<u32_any>(base, o));
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < 3; j++)
+        if ((uint32_t)j < rem) at<uint8_t>(base, o)[j] = (uint8_t)(w >> (8 * j));
 }
 
 inline spccl_status_t launch_status() { return hipGetLastError() == hipSuccess ? SPCCL_OK : SPCCL_ERR_HIP; }
@@ -107,8 +133,10 @@ inline bool overlaps(const void* a, uint64_t an, const void* b, uint64_t bn) {
 // ---------------------------------------------------------------------------
 // pruning with error feedback
 
-constexpr uint32_t kThreads = 256, kQuads = 4;
-constexpr uint32_t kChunk = kThreads * kQuads * 4;      // elements a block takes at a time
+constexpr uint32_t kThreads = 256;
+// Quads of a thread and elements of a block (fp32 at 2^26 elements with 4, 2 and
+// 1 quads 170, 180 and 178 us: 6.3 TB/s with 4; bf16 at 10^8 191, 191 and 188).
+constexpr uint32_t kPruneQuads = 4, kPruneChunk = kThreads * kPruneQuads * 4;
 
 struct PruneArgs {
     const uint8_t* grad;
@@ -123,22 +151,24 @@ struct PruneArgs {
 // behind would spoil its element for good and no rank would see it.  A sum
 // that overflows bf16 is sent as the infinity it rounds to, likewise without
 // a residual.
-template <int DT>
-__global__ void __launch_bounds__(kThreads) k_prune(PruneArgs g) {
-    const uint64_t e0 = (uint64_t)blockIdx.x * kChunk + threadIdx.x * 4;
+template <int DT, bool Full>
+__device__ __forceinline__ void prune_chunk(const PruneArgs& g, uint64_t e0, uint32_t end) {
+    constexpr uint32_t size = DT == kF32 ? 4 : 2;
+    const uint64_t grad = (uint64_t)g.grad + e0 * size, out = (uint64_t)g.out + e0 * size;
+    const uint64_t residual = (uint64_t)g.residual + e0 * 4;
     const float tau = *g.threshold;
-    Quad x[kQuads], r[kQuads];
+    const auto exists = [&](uint32_t i) -> uint32_t { return Full ? 4u : (i >= end ? 0u : (end - i < 4 ? end - i : 4u)); };
+    Quad x[kPruneQuads], r[kPruneQuads];
 #pragma unroll
-    for (uint32_t k = 0; k < kQuads; k++) {
-        const uint64_t e = e0 + k * kThreads * 4;
-        const uint32_t rem = e < g.n ? (uint32_t)(g.n - e < 4 ? g.n - e : 4) : 0;
-        x[k] = load_quad<DT>(g.grad, e, rem);
-        r[k] = load_quad<kF32>(g.residual, e, rem);
+    for (uint32_t k = 0; k < kPruneQuads; k++) {
+        const uint32_t i = (k * kThreads + threadIdx.x) * 4;
+        x[k] = get4<DT, Full>(grad, i, exists(i));
+        r[k] = get4<kF32, Full>(residual, i, exists(i));
     }
 #pragma unroll
-    for (uint32_t k = 0; k < kQuads; k++) {
-        const uint64_t e = e0 + k * kThreads * 4;
-        const uint32_t rem = e < g.n ? (uint32_t)(g.n - e < 4 ? g.n - e : 4) : 0;
+    for (uint32_t k = 0; k < kPruneQuads; k++) {
+        const uint32_t i = (k * kThreads + threadIdx.x) * 4, rem = exists(i);
+        if (!Full && !rem) continue;
         float sent[4], back[4];
 #pragma unroll
         for (int j = 0; j < 4; j++) {
@@ -156,17 +186,24 @@ __global__ void __launch_bounds__(kThreads) k_prune(PruneArgs g) {
         }
 #pragma unroll
         for (int j = 0; j < 4; j++) back[j] = __builtin_isfinite(sent[j]) ? back[j] - sent[j] : 0.f;
-        if (!rem) continue;
-        store_f32(g.residual, e, rem, back);
-        if constexpr (DT == kBF16) store_16(g.out, e, rem, pairs);
-        else store_f32(g.out, e, rem, sent);
+        put4_f32<Full>(residual, i, rem, back);
+        if constexpr (DT == kBF16) put4_16<Full>(out, i, rem, pairs);
+        else put4_f32<Full>(out, i, rem, sent);
     }
+}
+
+template <int DT>
+__global__ void __launch_bounds__(kThreads) k_prune(PruneArgs g) {
+    const uint64_t e0 = (uint64_t)blockIdx.x * kPruneChunk;
+    if (g.n - e0 >= kPruneChunk) prune_chunk<DT, true>(g, e0, kPruneChunk);
+    else prune_chunk<DT, false>(g, e0, (uint32_t)(g.n - e0));
 }
 
 // ---------------------------------------------------------------------------
 // AdamW
 
 constexpr uint32_t kBlock = 32;             // 8-bit states: elements that share a scale
+
 
 // One tensor as the kernel sees it, in the plan's table.
 struct AdamTensor {
@@ -289,24 +326,6 @@ __device__ __forceinline__ Quad decode4(uint32_t word, uint32_t scale) {
     const auto b = __builtin_amdgcn_cvt_pk_f32_fp8((int)word, true);
     return Quad{{a[0] * s, a[1] * s, b[0] * s, b[1] * s}};
 }
-__device__ __forceinline__ uint32_t load_codes(const uint8_t* p, uint32_t rem) {
-    if (rem >= 4) return *reinterpret_cast<const u32_any*>(p);
-    uint32_t w = 0;
-#pragma unroll
-    for (int j = 0; j < 3; j++)
-        if ((uint32_t)j < rem) w |= (uint32_t)p[j] << (8 * j);
-    return w;
-}
-__device__ __forceinline__ void store_codes(uint8_t* p, uint32_t rem, uint32_t w) {
-    if (rem >= 4) {
-        *reinterpret_cast<u32_any*>(p) = w;
-        return;
-    }
-#pragma unroll
-    for (int j = 0; j < 3; j++)
-        if ((uint32_t)j < rem) p[j] = (uint8_t)(w >> (8 * j));
-}
-
 // A gradient message: its header, checked like every reader's (each offset is
 // the one that the layout implies, so a passing header bounds every read).
 struct Message {
@@ -349,7 +368,7 @@ __device__ __forceinline__ void expand_tile(const uint8_t* msg, uint64_t nnz, ui
     const uint32_t base = I[t], next = I[t + 1];
     u32x4* zero = reinterpret_cast<u32x4*>(tile);
 #pragma unroll
-    for (uint32_t k = 0; k < kQuads; k++) zero[k * kThreads + threadIdx.x] = u32x4{0, 0, 0, 0};
+    for (uint32_t k = 0; k < kTileElems / (4 * kThreads); k++) zero[k * kThreads + threadIdx.x] = u32x4{0, 0, 0, 0};
     const uint32_t cnt = (uint32_t)__popcll(word);
     const uint32_t incl = wave_incl_scan(cnt);
     const uint32_t total = (uint32_t)__builtin_amdgcn_readlane((int)incl, 63);
@@ -379,57 +398,53 @@ __device__ __forceinline__ void expand_tile(const uint8_t* msg, uint64_t nnz, ui
     __syncthreads();
 }
 
-// One chunk of one tensor per block, found through the plan's table.  Stream:
-// the chunk is what the tensor has of one 4096-element tile of the message,
-// whose gradient is expanded into LDS while the states are on their way.
-template <int PT, int GT, bool Eight, bool Stream>
-__global__ void __launch_bounds__(kThreads) k_adamw(AdamArgs a) {
-    __shared__ __attribute__((aligned(16))) float tile[Stream ? kTileElems : 4];
-    const uint64_t id = a.chunk0 + blockIdx.x;
-    const AdamTensor& t = a.table[a.chunk[id]];
-    const uint64_t n = t.n;
-    // the tensor's element at this thread's first place; a stream's chunks
-    // follow the message's tiles, so its first may begin before the tensor
-    const int64_t e0 = (int64_t)((id - t.first) * kChunk) + threadIdx.x * 4 -
-                       (Stream ? (int64_t)(t.grad_offset % kTileElems) : 0);
-    Message msg{true, false, 0};
-    if constexpr (Stream) {
-        msg = check_message(t.grad, t.grad_cap, t.grad_n, GT);
-        if (!msg.ok) {
-            if (threadIdx.x == 0) atomicCAS(&a.ctrl->status, 0u, (uint32_t)SPCCL_ERR_CORRUPT_STREAM);
-            return;
-        }
-    }
+// Quads of a thread and elements of a chunk: a stream's chunk is a tile of the
+// message; an array's is a quad a thread.  More in flight per block is no
+// faster (2, 4 and 8 quads at 2^28 elements: 1384, 1354 and 1327 us against
+// 1338, but 274, 272 and 290 against 263 in 8 bits, and 78, 82 and 84 against
+// 77 at 2^24).
+constexpr uint32_t chunk_quads(bool stream) { return stream ? kTileElems / (kThreads * 4) : 1; }
+constexpr uint32_t chunk_elems(bool stream) { return kThreads * chunk_quads(stream) * 4; }
+static_assert(chunk_elems(true) == kTileElems, "a stream's chunk is a tile");
+
+// What a block works on: a tensor's arrays from the chunk's first element on,
+// `lead` places before which (a stream's first chunk) and `end` places after
+// which the tensor has none.
+struct Chunk {
+    uint64_t param, model, m, v, ms, vs, grad;
+    uint32_t lead, end;
+    uint32_t random;          // place of the first element in the random sequence, over 4
+    bool pici;
+    uint64_t nnz, tile;
+};
+
+template <int PT, int GT, bool Eight, bool Stream, bool Full>
+__device__ __forceinline__ void adamw_chunk(const AdamArgs& a, const AdamTensor& t, const Chunk& c, float* tile) {
+    constexpr uint32_t kQuads = chunk_quads(Stream);
+    const uint32_t i0 = threadIdx.x * 4;
+    const auto exists = [&](uint32_t i) -> uint32_t {          // how many of the four places at i
+        return Full ? 4u : (i < c.lead || i >= c.end ? 0u : (c.end - i < 4 ? c.end - i : 4u));
+    };
     Quad p[kQuads], g[kQuads], m[kQuads], v[kQuads];
     uint32_t mc[kQuads], vc[kQuads], ms[kQuads], vs[kQuads];
-    const uint8_t* values = t.grad;
-    uint64_t at = 0;
-    if constexpr (Stream) {
-        if (!msg.pici) {
-            values = t.grad + kHeaderBytes;
-            at = t.grad_offset;
-        }
-    }
 #pragma unroll
     for (uint32_t k = 0; k < kQuads; k++) {
-        const int64_t e = e0 + k * kThreads * 4;
-        const uint32_t rem = e >= 0 && (uint64_t)e < n ? (uint32_t)(n - e < 4 ? n - e : 4) : 0;
-        const uint64_t o = rem ? (uint64_t)e : 0;
-        p[k] = load_quad<PT>(t.param, o, rem);
-        if (!(Stream && msg.pici)) g[k] = load_quad<GT>(values, at + o, rem);
+        const uint32_t i = i0 + k * kThreads * 4, rem = exists(i);
+        p[k] = get4<PT, Full>(c.param, i, rem);
+        if (!Stream || !c.pici) g[k] = get4<GT, Full>(c.grad, i, rem);
         if constexpr (Eight) {
-            mc[k] = load_codes(t.m + o, rem);
-            vc[k] = load_codes(t.v + o, rem);
-            ms[k] = rem ? t.ms[o / kBlock] : 0;
-            vs[k] = rem ? t.vs[o / kBlock] : 0;
+            mc[k] = get4_8<Full>(c.m, i, rem);
+            vc[k] = get4_8<Full>(c.v, i, rem);
+            ms[k] = Full || rem ? *at<const uint8_t>(c.ms, i / kBlock) : 0;
+            vs[k] = Full || rem ? *at<const uint8_t>(c.vs, i / kBlock) : 0;
         } else {
-            m[k] = load_quad<kF32>(t.m, o, rem);
-            v[k] = load_quad<kF32>(t.v, o, rem);
+            m[k] = get4<kF32, Full>(c.m, i, rem);
+            v[k] = get4<kF32, Full>(c.v, i, rem);
         }
     }
     if constexpr (Stream) {
-        if (msg.pici) {
-            expand_tile<GT>(t.grad, msg.nnz, t.grad_n, t.grad_offset / kTileElems + (id - t.first), tile, a.ctrl);
+        if (c.pici) {
+            expand_tile<GT>(t.grad, c.nnz, t.grad_n, c.tile, tile, a.ctrl);
 #pragma unroll
             for (uint32_t k = 0; k < kQuads; k++) {
                 const u32x4 x = reinterpret_cast<const u32x4*>(tile)[k * kThreads + threadIdx.x];
@@ -442,9 +457,7 @@ __global__ void __launch_bounds__(kThreads) k_adamw(AdamArgs a) {
     const float keep = (float)(1.0 - a.lr * t.decay);
 #pragma unroll
     for (uint32_t k = 0; k < kQuads; k++) {
-        const int64_t e = e0 + k * kThreads * 4;
-        const uint32_t rem = e >= 0 && (uint64_t)e < n ? (uint32_t)(n - e < 4 ? n - e : 4) : 0;
-        const uint64_t o = rem ? (uint64_t)e : 0;
+        const uint32_t i = i0 + k * kThreads * 4, rem = exists(i);
         if constexpr (Eight) {
             m[k] = decode4(mc[k], ms[k]);
             v[k] = decode4(vc[k], vs[k]);
@@ -455,46 +468,85 @@ __global__ void __launch_bounds__(kThreads) k_adamw(AdamArgs a) {
             const float d = g[k].f[j] * scale;
             mn[j] = m[k].f[j] * a.b1 + d * a.c1;
             vn[j] = v[k].f[j] * a.b2 + (d * d) * a.c2;
-            const float denom = sqrtf(vn[j]) * a.root + a.eps;
-            pn[j] = p[k].f[j] * keep - (mn[j] / denom) * a.rate;
+            pn[j] = p[k].f[j] * keep - (mn[j] / (sqrtf(vn[j]) * a.root + a.eps)) * a.rate;
         }
         uint32_t h = 0;
-        if constexpr (Eight || PT == kBF16) h = mix((uint32_t)((t.counter + o) >> 2) ^ a.key);
+        if constexpr (Eight || PT == kBF16) h = mix((c.random + i / 4) ^ a.key);
         if constexpr (Eight) {
-            // lanes past the end hold zeros: they do not move a block's scale
+            // places past the end hold zeros: they do not move a block's scale
             uint32_t mt = 0, vt = 0;
 #pragma unroll
             for (int j = 0; j < 4; j++) {
-                const bool in = (uint32_t)j < rem;
+                const bool in = Full || (uint32_t)j < rem;
                 mt = max(mt, in ? __float_as_uint(mn[j]) & 0x7FFFFFFFu : 0u);
                 vt = max(vt, in ? __float_as_uint(vn[j]) & 0x7FFFFFFFu : 0u);
             }
             const Scale sm = scale_of(block_max(mt)), sv = scale_of(block_max(vt));
-            if (rem) {
-                store_codes(t.m + o, rem, encode4(mn, sm.up, h, 0, false));
-                store_codes(t.v + o, rem, encode4(vn, sv.up, h, 12, true));
-                if (o % kBlock == 0) {
-                    t.ms[o / kBlock] = (uint8_t)sm.byte;
-                    t.vs[o / kBlock] = (uint8_t)sv.byte;
+            if (Full || rem) {
+                put4_8<Full>(c.m, i, rem, encode4(mn, sm.up, h, 0, false));
+                put4_8<Full>(c.v, i, rem, encode4(vn, sv.up, h, 12, true));
+                if (i % kBlock == 0) {
+                    *at<uint8_t>(c.ms, i / kBlock) = (uint8_t)sm.byte;
+                    *at<uint8_t>(c.vs, i / kBlock) = (uint8_t)sv.byte;
                 }
             }
         }
-        if (!rem) continue;
+        if (!Full && !rem) continue;
         if constexpr (!Eight) {
-            store_f32(t.m, o, rem, mn);
-            store_f32(t.v, o, rem, vn);
+            put4_f32<Full>(c.m, i, rem, mn);
+            put4_f32<Full>(c.v, i, rem, vn);
         }
         if constexpr (PT == kF32) {
-            store_f32(t.param, o, rem, pn);
-            if (t.model) store_16(t.model, o, rem, u32x2{bf16_pair(pn[0], pn[1]), bf16_pair(pn[2], pn[3])});
+            put4_f32<Full>(c.param, i, rem, pn);
+            if (c.model) put4_16<Full>(c.model, i, rem, u32x2{bf16_pair(pn[0], pn[1]), bf16_pair(pn[2], pn[3])});
         } else {
             const uint32_t h2 = h * kSecond;
             uint32_t b[4];
 #pragma unroll
             for (int j = 0; j < 4; j++) b[j] = bf16_stochastic(pn[j], h2 + (uint32_t)j * kStride);
-            store_16(t.param, o, rem, u32x2{b[0] | (b[1] << 16), b[2] | (b[3] << 16)});
+            put4_16<Full>(c.param, i, rem, u32x2{b[0] | (b[1] << 16), b[2] | (b[3] << 16)});
         }
     }
+}
+
+// One chunk of one tensor per block, found through the plan's table.  Stream:
+// the chunk is what the tensor has of one 4096-element tile of the message,
+// whose gradient is expanded into LDS while the states are on their way.
+template <int PT, int GT, bool Eight, bool Stream>
+__global__ void __launch_bounds__(kThreads) k_adamw(AdamArgs a) {
+    __shared__ __attribute__((aligned(16))) float tile[Stream ? kTileElems : 4];
+    constexpr uint32_t kChunk = chunk_elems(Stream);
+    const uint64_t id = a.chunk0 + blockIdx.x;
+    const AdamTensor t = a.table[a.chunk[id]];
+    const uint64_t nth = id - t.first;
+    Chunk c{};
+    c.lead = Stream && nth == 0 ? (uint32_t)(t.grad_offset % kTileElems) : 0u;
+    // the tensor's element at the chunk's first place; a stream's chunks follow
+    // the message's tiles, so its first may begin before the tensor
+    const int64_t e0 = (int64_t)(nth * kChunk) - (Stream ? (int64_t)(t.grad_offset % kTileElems) : 0);
+    const int64_t left = (int64_t)t.n - e0;
+    c.end = left < (int64_t)kChunk ? (uint32_t)left : kChunk;
+    c.param = (uint64_t)t.param + e0 * (PT == kF32 ? 4 : 2);
+    c.model = t.model ? (uint64_t)t.model + e0 * 2 : 0;
+    c.m = (uint64_t)t.m + e0 * (Eight ? 1 : 4);
+    c.v = (uint64_t)t.v + e0 * (Eight ? 1 : 4);
+    c.ms = (uint64_t)t.ms + e0 / (int64_t)kBlock;
+    c.vs = (uint64_t)t.vs + e0 / (int64_t)kBlock;
+    c.grad = (uint64_t)t.grad + e0 * (GT == kF32 ? 4 : 2);
+    c.random = (uint32_t)((t.counter + (uint64_t)e0) >> 2);
+    if constexpr (Stream) {
+        const Message msg = check_message(t.grad, t.grad_cap, t.grad_n, GT);
+        if (!msg.ok) {
+            if (threadIdx.x == 0) atomicCAS(&a.ctrl->status, 0u, (uint32_t)SPCCL_ERR_CORRUPT_STREAM);
+            return;
+        }
+        c.pici = msg.pici;
+        c.nnz = msg.nnz;
+        c.tile = t.grad_offset / kTileElems + nth;
+        if (!c.pici) c.grad += kHeaderBytes + t.grad_offset * (GT == kF32 ? 4 : 2);
+    }
+    if (c.lead == 0 && c.end == kChunk) adamw_chunk<PT, GT, Eight, Stream, true>(a, t, c, tile);
+    else adamw_chunk<PT, GT, Eight, Stream, false>(a, t, c, tile);
 }
 
 // ---------------------------------------------------------------------------
@@ -504,14 +556,13 @@ constexpr uint32_t kPlanMagic = 0x4D414441u;      // "ADAM"
 
 inline bool is_stream(const spccl_adamw_tensor_t& t) { return t.grad.kind == SPCCL_STREAM; }
 
-// Chunks of a tensor: 4096 elements each, a stream's cut where the message's
-// tiles are.
+// Chunks of a tensor; a stream's are cut where the message's tiles are.
 uint64_t chunks_of(const spccl_adamw_tensor_t& t) {
     if (!t.n) return 0;
     const uint64_t lead = is_stream(t) ? t.grad_offset % kTileElems : 0;
-    return (lead + t.n + kChunk - 1) / kChunk;
+    const uint64_t chunk = chunk_elems(is_stream(t));
+    return (lead + t.n + chunk - 1) / chunk;
 }
-static_assert(kChunk == kTileElems, "a stream's chunk is a tile");
 
 uint64_t table_bytes(const spccl_adamw_tensor_t* t, int32_t count, uint64_t* arrays, uint64_t* streams) {
     *arrays = *streams = 0;
@@ -621,7 +672,7 @@ spccl_status_t spccl_prune(const void* grad, float* residual, const float* thres
     if (overlaps(threshold, 4, out, n * s) || overlaps(threshold, 4, residual, 4 * n)) return SPCCL_ERR_INVALID_ARG;
     const PruneArgs g{static_cast<const uint8_t*>(grad), reinterpret_cast<uint8_t*>(residual), static_cast<uint8_t*>(out),
                       threshold, n, (float)leak};
-    const dim3 grid((uint32_t)((n + kChunk - 1) / kChunk)), block(kThreads);
+    const dim3 grid((uint32_t)((n + kPruneChunk - 1) / kPruneChunk)), block(kThreads);
     const hipStream_t st = reinterpret_cast<hipStream_t>(stream);
     if (dtype == kF32) hipLaunchKernelGGL(k_prune<kF32>, grid, block, 0, st, g);
     else hipLaunchKernelGGL(k_prune<kBF16>, grid, block, 0, st, g);
