@@ -118,6 +118,105 @@ __device__ __forceinline__ void load_param(const uint8_t* base, uint32_t c, uint
     }
 }
 
+// A lane's vector of a row that lies whole in registers: columns [a, a + vec),
+// of which those before `first` are another lane's or do not exist.  Every
+// load is one full vector inside the row, without a branch (a load in a branch
+// is waited for at the branch's end, before the next can issue): a lane past
+// the end reads the row's last vector for nothing, and where the row's length
+// is no multiple of vec (Ragged), its last vector is read from vec columns
+// before its end.
+template <class E, bool Ragged>
+struct Place {
+    uint32_t a, first;
+    __device__ __forceinline__ Place(uint32_t c, uint32_t cols) {
+        if constexpr (Ragged) {
+            a = c + E::vec <= cols ? c : cols - E::vec;
+            first = c + E::vec <= cols ? 0 : (c >= cols ? E::vec : c + E::vec - cols);
+            asm("" : "+v"(first));         // masks of its values are made where they are used, not kept
+        } else {
+            a = c < cols ? c : cols - E::vec;
+            first = c < cols ? 0 : E::vec;
+        }
+    }
+    __device__ __forceinline__ bool any() const { return first < (uint32_t)E::vec; }
+    // zeros in the elements before `first`
+    __device__ __forceinline__ void clear(u32x4& v) const {
+        constexpr int per = 4 / sizeof(typename E::raw);
+#pragma unroll
+        for (int q = 0; q < 4; q++) {
+            if constexpr (!Ragged)
+                v[q] = any() ? v[q] : 0u;
+            else if constexpr (per == 2)
+                v[q] = first >= (uint32_t)(2 * q + 2) ? 0u : (first == (uint32_t)(2 * q + 1) ? v[q] & 0xFFFF0000u : v[q]);
+            else
+                v[q] = first > (uint32_t)q ? 0u : v[q];
+        }
+    }
+    __device__ __forceinline__ void store(uint8_t* row, const float* f) const {
+        using raw = typename E::raw;
+        if (first == 0) {
+            __builtin_nontemporal_store(E::pack(f), reinterpret_cast<typename E::vec_any*>(row + a * (uint32_t)sizeof(raw)));
+            return;
+        }
+        if constexpr (Ragged) {
+            raw* p = reinterpret_cast<raw*>(row) + a;
+#pragma unroll
+            for (int j = 1; j < E::vec; j++)
+                if ((uint32_t)j >= first) p[j] = E::round(f[j]);
+        }
+    }
+};
+template <class E, bool Stream>
+__device__ __forceinline__ u32x4 load_row(const uint8_t* row, uint32_t a) {
+    const auto* p = reinterpret_cast<const typename E::vec_any*>(row + a * (uint32_t)sizeof(typename E::raw));
+    if constexpr (Stream) return __builtin_nontemporal_load(p);
+    else return *p;
+}
+
+// A row's weights or biases at a lane's places, as they are stored: all loads
+// issue before the first is converted.  absent: the bits of a null array.
+template <class E, class W, int K>
+struct Params {
+    static constexpr int D = E::vec * sizeof(typename W::raw) / 4;     // words per vector: 2, 4 or 8
+    uint32_t r[K][D];
+    __device__ __forceinline__ void load(const uint8_t* base, const uint32_t (&a)[K], float absent) {
+        if (base) {
+#pragma unroll
+            for (int k = 0; k < K; k++) {
+                const uint8_t* p = base + a[k] * (uint32_t)sizeof(typename W::raw);
+                if constexpr (D == 2) {
+                    typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+                    typedef u32x2 __attribute__((aligned(2))) half_any;
+                    const u32x2 v = *reinterpret_cast<const half_any*>(p);
+                    r[k][0] = v[0];
+                    r[k][1] = v[1];
+                } else {
+#pragma unroll
+                    for (int q = 0; q < D / 4; q++) {
+                        const u32x4 v = reinterpret_cast<const typename W::vec_any*>(p)[q];
+#pragma unroll
+                        for (int z = 0; z < 4; z++) r[k][4 * q + z] = v[z];
+                    }
+                }
+            }
+        } else {
+            const uint32_t one = sizeof(typename W::raw) == 4 ? W::round(absent) : W::round(absent) * 0x10001u;
+#pragma unroll
+            for (int k = 0; k < K; k++)
+#pragma unroll
+                for (int z = 0; z < D; z++) r[k][z] = one;
+        }
+    }
+    __device__ __forceinline__ void pin(int k) {
+#pragma unroll
+        for (int z = 0; z < D; z++) asm volatile("" : "+v"(r[k][z]));
+    }
+    __device__ __forceinline__ float get(int k, int j) const {
+        if constexpr (sizeof(typename W::raw) == 4) return __uint_as_float(r[k][j]);
+        else return __uint_as_float(j & 1 ? r[k][j / 2] & 0xFFFF0000u : r[k][j / 2] << 16);
+    }
+};
+
 // ---------------------------------------------------------------------------
 // sums over the lanes of a row
 
@@ -147,14 +246,19 @@ __device__ __forceinline__ float lanes_sum(float x) {
 
 // How a row lies over lanes: L lanes of one wave (Waves = 1) or all lanes of
 // Waves waves, K vectors each; vector k of lane i is vector k * lanes + i.
-template <class E, int L, int Waves, int K>
+template <class E, int L, int Waves, int K, uint32_t Threads = 256>
 struct Row {
     static_assert(Waves == 1 || L == 64, "a row is part of a wave, or whole waves");
     static constexpr uint32_t lanes = L * Waves;
     static constexpr uint32_t cap = lanes * K * E::vec;           // columns that fit
-    static constexpr uint32_t threads = Waves > 4 ? 64 * Waves : 256;
+    static constexpr uint32_t threads = 64 * Waves > Threads ? 64 * Waves : Threads;
     static constexpr uint32_t rows = threads / lanes;             // rows of a block at a time
     static constexpr uint32_t waves = threads / 64;
+    // the thread's row of the block; whole waves know it as a scalar
+    static __device__ __forceinline__ uint32_t group() {
+        if constexpr (L == 64) return (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)) / Waves;
+        else return threadIdx.x / lanes;
+    }
 };
 
 struct LnArgs {
@@ -175,28 +279,41 @@ struct LnArgs {
 // row spans waves, each takes the mean and the squared deviations of its own
 // columns and the waves' are joined (n1 m1 + n2 m2; the squared distance of a
 // part's mean from the whole's counts for each of its columns), so a row
-// meets one barrier.
-template <class E, class W, int L, int Waves, int K>
+// meets one barrier.  A row of one wave reads its weights along with x; a
+// longer one afterwards, as their registers would cost it waves (32768 x 8192
+// bf16: 181 us against 194; 16384 x 1024: 11.3 early, 12.1 late).  Stores
+// are non-temporal, loads are not (10007 x 1600 fp32: 20.4 us; 27.1 with
+// ordinary stores, 25.4 with non-temporal loads too).  65536 x 4096 of either
+// type and 32768 x 8192 bf16 run at 5.9 TB/s.
+template <class E, class W, int L, int Waves, int K, bool Ragged>
 __global__ void __launch_bounds__((Row<E, L, Waves, K>::threads)) k_layer_norm(LnArgs g) {
     using R = Row<E, L, Waves, K>;
+    using At = Place<E, Ragged>;
     constexpr int V = E::vec;
     const uint32_t i = threadIdx.x % R::lanes;                    // lane of the row
-    const uint32_t group = threadIdx.x / R::lanes;
+    const uint32_t group = R::group();
     const uint64_t row = (uint64_t)blockIdx.x * R::rows + group;
     const bool mine = row < g.rows;
     const uint8_t* src = g.x + (mine ? row : 0) * g.ldx;
+    uint32_t a[K];
     u32x4 v[K];
 #pragma unroll
     for (int k = 0; k < K; k++) {
-        const uint32_t c = (k * R::lanes + i) * V;
-        const uint32_t rem = mine && c < g.cols ? g.cols - c : 0;
-        v[k] = load_vec<E>(src, c, rem);
+        a[k] = At((k * R::lanes + i) * V, g.cols).a;
+        v[k] = load_row<E, false>(src, a[k]);
+    }
+    Params<E, W, K> w, b;
+    if constexpr (Waves == 1) {
+        w.load(g.w, a, 1.f);
+        b.load(g.b, a, 0.f);
     }
     float sum = 0.f;
 #pragma unroll
-    for (int k = 0; k < K; k++)
+    for (int k = 0; k < K; k++) {
+        At((k * R::lanes + i) * V, g.cols).clear(v[k]);
 #pragma unroll
         for (int j = 0; j < V; j++) sum += E::get(v[k], j);
+    }
     // the columns whose mean is taken first: the row's, or this wave's part
     uint32_t n = g.cols;
     if constexpr (Waves > 1) {
@@ -211,21 +328,14 @@ __global__ void __launch_bounds__((Row<E, L, Waves, K>::threads)) k_layer_norm(L
     float dev = 0.f;
 #pragma unroll
     for (int k = 0; k < K; k++) {
-        const uint32_t c = (k * R::lanes + i) * V;
-        const uint32_t rem = c < g.cols ? g.cols - c : 0;
-        if (rem >= (uint32_t)V) {
+        const At at((k * R::lanes + i) * V, g.cols);
+        float part = 0.f;
 #pragma unroll
-            for (int j = 0; j < V; j++) {
-                const float d = E::get(v[k], j) - mean;
-                dev = fmaf(d, d, dev);
-            }
-        } else if (rem) {
-#pragma unroll
-            for (int j = 0; j < V - 1; j++) {
-                const float d = (uint32_t)j < rem ? E::get(v[k], j) - mean : 0.f;
-                dev = fmaf(d, d, dev);
-            }
+        for (int j = 0; j < V; j++) {
+            const float d = !Ragged || (uint32_t)j >= at.first ? E::get(v[k], j) - mean : 0.f;
+            part = fmaf(d, d, part);
         }
+        dev += at.any() ? part : 0.f;
     }
     dev = lanes_sum<L>(dev);
     if constexpr (Waves > 1) {
@@ -256,22 +366,24 @@ __global__ void __launch_bounds__((Row<E, L, Waves, K>::threads)) k_layer_norm(L
         if (g.rstd) g.rstd[row] = rstd;
     }
     uint8_t* dst = g.y + row * g.ldy;
+    if constexpr (Waves > 1) {
+#pragma unroll
+        for (int k = 0; k < K; k++) asm volatile("" : "+v"(a[k]));    // not earlier
+        w.load(g.w, a, 1.f);
+        b.load(g.b, a, 0.f);
+    }
 #pragma unroll
     for (int k = 0; k < K; k++) {
-        const uint32_t c = (k * R::lanes + i) * V;
-        if (c >= g.cols) break;
-        const uint32_t rem = g.cols - c;
-        float w[V], b[V], y[V];
-        load_param<W, V>(g.w, c, rem, 1.f, w);
-        load_param<W, V>(g.b, c, rem, 0.f, b);
+        float y[V];
 #pragma unroll
-        for (int j = 0; j < V; j++) y[j] = fmaf((E::get(v[k], j) - mean) * rstd, w[j], b[j]);
-        store_vec<E>(dst, c, rem, y);
+        for (int j = 0; j < V; j++) y[j] = fmaf((E::get(v[k], j) - mean) * rstd, w.get(k, j), b.get(k, j));
+        At((k * R::lanes + i) * V, g.cols).store(dst, y);
     }
 }
 
-// Rows too long for the registers of a block: the block reads its row three
-// times (its L2 holds it from the first), for the mean, the deviations and y.
+// Rows too long for the registers of a block, or shorter than a vector: the
+// block reads its row three times (the L2 holds it from the first), for the
+// mean, the deviations and y.
 template <class E, class W>
 __global__ void __launch_bounds__(1024) k_layer_norm_long(LnArgs g) {
     constexpr int V = E::vec;
@@ -338,63 +450,89 @@ struct LnBackArgs {
     uint32_t cols;
 };
 
+constexpr uint32_t kBackThreads = 512;
+
 // Each group of lanes walks over rows, keeping its columns' sums of dy h and
 // dy in registers; a block joins its groups' through LDS, in their order, and
 // leaves one pair of sums per column for k_layer_norm_grads, so no sum depends
-// on which block comes first.
-template <class E, class W, int L, int Waves, int K>
-__global__ void __launch_bounds__((Row<E, L, Waves, K>::threads)) k_layer_norm_back(LnBackArgs g) {
-    using R = Row<E, L, Waves, K>;
+// on which block comes first.  All accesses are non-temporal (65536 x 4096
+// bf16, 1.6 GB: 268 us, 6.0 TB/s; 288 with ordinary loads).
+template <class E, class W, int L, int Waves, int K, bool Ragged>
+__global__ void __launch_bounds__((Row<E, L, Waves, K, kBackThreads>::threads)) k_layer_norm_back(LnBackArgs g) {
+    using R = Row<E, L, Waves, K, kBackThreads>;
+    using At = Place<E, Ragged>;
     constexpr int V = E::vec;
     __shared__ float s_sum[R::rows > 1 ? R::cap : 1];
     __shared__ float s_row[2][2][R::waves];
     const uint32_t i = threadIdx.x % R::lanes;
-    const uint32_t group = threadIdx.x / R::lanes;
+    const uint32_t group = R::group();
     const uint32_t wave = threadIdx.x >> 6;
     float dw[K][V], db[K][V];
 #pragma unroll
     for (int k = 0; k < K; k++)
 #pragma unroll
         for (int j = 0; j < V; j++) dw[k][j] = db[k][j] = 0.f;
+    uint32_t a[K];
+#pragma unroll
+    for (int k = 0; k < K; k++) a[k] = At((k * R::lanes + i) * V, g.cols).a;
+    Params<E, W, K> w;
+    w.load(g.w, a, 1.f);
     const float inv = 1.0f / (float)g.cols;
-    uint32_t turn = 0;
-    for (uint64_t r0 = (uint64_t)blockIdx.x * R::rows; r0 < g.rows; r0 += (uint64_t)gridDim.x * R::rows, turn ^= 1) {
-        const uint64_t row = r0 + group;
-        const bool mine = row < g.rows;
-        const uint64_t at = mine ? row : 0;
-        const uint8_t* px = g.x + at * g.ldx;
-        const uint8_t* pdy = g.dy + at * g.lddy;
+    // a row's data; a group past the last row takes the last one along
+    struct Data {
         u32x4 x[K], dy[K];
+        float mean, rstd;
+    };
+    const auto fetch = [&](uint64_t r0, Data& d) {
+        const uint64_t row = r0 + group < g.rows ? r0 + group : g.rows - 1;
+        const uint8_t* px = g.x + row * g.ldx;
+        const uint8_t* pdy = g.dy + row * g.lddy;
 #pragma unroll
         for (int k = 0; k < K; k++) {
-            const uint32_t c = (k * R::lanes + i) * V;
-            const uint32_t rem = mine && c < g.cols ? g.cols - c : 0;
-            x[k] = load_vec<E>(px, c, rem);
-            dy[k] = load_vec<E>(pdy, c, rem);
+            d.x[k] = load_row<E, true>(px, a[k]);
+            d.dy[k] = load_row<E, true>(pdy, a[k]);
         }
-        const float mean = mine ? g.mean[at] : 0.f, rstd = mine ? g.rstd[at] : 0.f;
-        // an opaque column: the weight is read again for each row (it stays in
-        // the caches) instead of held in registers over all of them
-        uint32_t ci = i * V;
-        asm volatile("" : "+v"(ci));
+        d.mean = g.mean[row];
+        d.rstd = g.rstd[row];
+    };
+    // the next row is on its way while this one is worked on, where the
+    // registers for it are there (1024 threads have 128 each)
+    constexpr bool Ahead = R::threads <= 512 || K <= 2;
+    const uint64_t step = (uint64_t)gridDim.x * R::rows;
+    uint32_t turn = 0;
+    Data next;
+    if constexpr (Ahead) fetch((uint64_t)blockIdx.x * R::rows, next);
+    for (uint64_t r0 = (uint64_t)blockIdx.x * R::rows; r0 < g.rows; r0 += step, turn ^= 1) {
+        Data now;
+        if constexpr (Ahead) {
+            now = next;
+            fetch(r0 + step, next);
+        } else {
+            fetch(r0, now);
+        }
+        const bool mine = R::rows == 1 || r0 + group < g.rows;
+        const uint64_t row = r0 + group;
+        auto& x = now.x;
+        auto& dy = now.dy;
+        const float mean = now.mean, rstd = now.rstd;
         float s1 = 0.f, s2 = 0.f;
 #pragma unroll
         for (int k = 0; k < K; k++) {
-            const uint32_t c = k * R::lanes * V + ci;
-            float w[V];
-            load_param<W, V>(g.w, c, c < g.cols ? g.cols - c : 0, 1.f, w);
+            w.pin(k);
+            At((k * R::lanes + i) * V, mine ? g.cols : 0).clear(dy[k]);
 #pragma unroll
             for (int j = 0; j < V; j++) {
                 const float d = E::get(dy[k], j);
                 const float h = (E::get(x[k], j) - mean) * rstd;
-                const float t = d * w[j];
+                const float t = d * w.get(k, j);
                 s1 = fmaf(t, h, s1);
                 s2 += t;
                 dw[k][j] = fmaf(d, h, dw[k][j]);
                 db[k][j] += d;
+                asm volatile("" : "+v"(dw[k][j]), "+v"(db[k][j]));
             }
+            __builtin_amdgcn_sched_barrier(0);
         }
-        if (!g.dx) continue;
         s1 = lanes_sum<L>(s1);
         s2 = lanes_sum<L>(s2);
         if constexpr (Waves > 1) {
@@ -413,20 +551,22 @@ __global__ void __launch_bounds__((Row<E, L, Waves, K>::threads)) k_layer_norm_b
         }
         s1 *= inv;
         s2 *= inv;
-        if (!mine) continue;
+        // converted again below: what the first pass made of x and dy would
+        // otherwise stay in registers, four times what they take as stored
+#pragma unroll
+        for (int k = 0; k < K; k++) asm volatile("" : "+v"(x[k]), "+v"(dy[k]));
         uint8_t* dst = g.dx + row * g.lddx;
 #pragma unroll
         for (int k = 0; k < K; k++) {
-            const uint32_t c = k * R::lanes * V + ci;
-            if (c >= g.cols) break;
-            float w[V], o[V];
-            load_param<W, V>(g.w, c, g.cols - c, 1.f, w);
+            float o[V];
 #pragma unroll
             for (int j = 0; j < V; j++) {
                 const float h = (E::get(x[k], j) - mean) * rstd;
-                o[j] = fmaf(-h, s1, fmaf(E::get(dy[k], j), w[j], -s2)) * rstd;
+                o[j] = fmaf(-h, s1, fmaf(E::get(dy[k], j), w.get(k, j), -s2)) * rstd;
             }
-            store_vec<E>(dst, c, g.cols - c, o);
+            const At at((k * R::lanes + i) * V, g.cols);
+            if (mine && g.dx && at.any()) at.store(dst, o);
+            __builtin_amdgcn_sched_barrier(0);
         }
     }
     if (!g.part) return;
@@ -435,33 +575,39 @@ __global__ void __launch_bounds__((Row<E, L, Waves, K>::threads)) k_layer_norm_b
     for (int which = 0; which < 2; which++) {
         float(&acc)[K][V] = which ? db : dw;
         if constexpr (R::rows > 1) {
+            // a place per lane and element, the same for every group
             for (uint32_t q = 0; q < R::rows; q++) {
                 __syncthreads();
-                if (group == q) {
+                if (group != q) continue;
 #pragma unroll
-                    for (int k = 0; k < K; k++)
+                for (int k = 0; k < K; k++)
 #pragma unroll
-                        for (int j = 0; j < V; j++) {
-                            const uint32_t c = (k * R::lanes + i) * V + j;
-                            s_sum[c] = q ? s_sum[c] + acc[k][j] : acc[k][j];
-                        }
-                }
+                    for (int j = 0; j < V; j++) {
+                        float& sum = s_sum[(k * V + j) * R::lanes + i];
+                        sum = q ? sum + acc[k][j] : acc[k][j];
+                    }
             }
             __syncthreads();
-            for (uint32_t c = threadIdx.x; c < g.cols; c += R::threads) part[which * g.cols + c] = s_sum[c];
-        } else {
+            if (group == 0) {
 #pragma unroll
-            for (int k = 0; k < K; k++)
+                for (int k = 0; k < K; k++)
 #pragma unroll
-                for (int j = 0; j < V; j++) {
-                    const uint32_t c = (k * R::lanes + i) * V + j;
-                    if (c < g.cols) part[which * g.cols + c] = acc[k][j];
-                }
+                    for (int j = 0; j < V; j++) acc[k][j] = s_sum[(k * V + j) * R::lanes + i];
+            }
+        }
+        if (group == 0) {
+#pragma unroll
+            for (int k = 0; k < K; k++) {
+                const At at((k * R::lanes + i) * V, g.cols);
+#pragma unroll
+                for (int j = 0; j < V; j++)
+                    if ((uint32_t)j >= at.first) part[which * g.cols + at.a + j] = acc[k][j];
+            }
         }
     }
 }
 
-// Long rows: dx of one row per block, reading the row twice.
+// Long or very short rows: dx of one row per block, reading the row twice.
 template <class E, class W>
 __global__ void __launch_bounds__(1024) k_layer_norm_back_long(LnBackArgs g) {
     constexpr int V = E::vec;
@@ -512,7 +658,7 @@ __global__ void __launch_bounds__(1024) k_layer_norm_back_long(LnBackArgs g) {
 }
 
 // Sums of dy h and dy over a strip of rows (grid y), a vector of columns per
-// thread: the long rows' form of k_layer_norm_back's second result.
+// thread: k_layer_norm_back's second result for long or very short rows.
 template <class E>
 __global__ void __launch_bounds__(64) k_layer_norm_columns(LnBackArgs g) {
     constexpr int V = E::vec;
@@ -597,9 +743,11 @@ bool span_overlap(const void* p, uint64_t pn, const Rows& m, uint64_t rows, uint
 }
 
 // The layout of a row: lanes of a wave, or waves, and vectors per lane; calls
-// fn with the three as constants.  A block of 16 waves has 128 registers for
-// each lane: enough for a forward row of 32 elements, not for the backward
-// pass's rows and sums.
+// fn with the three as constants.  Short rows take 8 elements a lane; from 513
+// columns on a wave's own row takes 16, then 32 (16384 x 1600 bf16: 16.5 us,
+// 17.3 with two waves of 16; 16384 x 1024: 13.8 and 11.3).  The backward pass
+// holds two sums for each element, so its rows take 16 and spread over waves
+// sooner (32: 65536 x 1024 88 us against 74, 65536 x 4096 283 against 268).
 constexpr uint32_t kMaxCols = 32768, kMaxBackCols = 16384;       // beyond: the long forms
 
 template <int N>
@@ -607,34 +755,45 @@ using Int = std::integral_constant<int, N>;
 
 template <class E, bool Back, class Fn>
 auto with_row(uint32_t cols, Fn fn) {
-    constexpr int K1 = 8 / E::vec, K4 = 32 / E::vec;              // 8 and 32 elements per lane
-    if (cols <= 8 * 8) return fn(Int<8>{}, Int<1>{}, Int<K1>{});
-    if (cols <= 16 * 8) return fn(Int<16>{}, Int<1>{}, Int<K1>{});
-    if (cols <= 32 * 8) return fn(Int<32>{}, Int<1>{}, Int<K1>{});
-    if (cols <= 64 * 8) return fn(Int<64>{}, Int<1>{}, Int<K1>{});
-    if (cols <= 64 * 32) return fn(Int<64>{}, Int<1>{}, Int<K4>{});
-    if (cols <= 64 * 32 * 2) return fn(Int<64>{}, Int<2>{}, Int<K4>{});
-    if (cols <= 64 * 32 * 4) return fn(Int<64>{}, Int<4>{}, Int<K4>{});
-    if (Back || cols <= 64 * 32 * 8) return fn(Int<64>{}, Int<8>{}, Int<K4>{});
-    if constexpr (!Back) return fn(Int<64>{}, Int<16>{}, Int<K4>{});
+    constexpr int K8 = 8 / E::vec, K16 = 16 / E::vec, K32 = 32 / E::vec;
+    if (cols <= 64) return fn(Int<8>{}, Int<1>{}, Int<K8>{});
+    if (cols <= 128) return fn(Int<16>{}, Int<1>{}, Int<K8>{});
+    if (cols <= 256) return fn(Int<32>{}, Int<1>{}, Int<K8>{});
+    if (cols <= 512) return fn(Int<64>{}, Int<1>{}, Int<K8>{});
+    if (cols <= 1024) return fn(Int<64>{}, Int<1>{}, Int<K16>{});
+    if constexpr (Back) {
+        if (cols <= 2048) return fn(Int<64>{}, Int<2>{}, Int<K16>{});
+        if (cols <= 4096) return fn(Int<64>{}, Int<4>{}, Int<K16>{});
+        if (cols <= 8192) return fn(Int<64>{}, Int<8>{}, Int<K16>{});
+        return fn(Int<64>{}, Int<16>{}, Int<K16>{});
+    } else {
+        if (cols <= 2048) return fn(Int<64>{}, Int<1>{}, Int<K32>{});
+        if (cols <= 4096) return fn(Int<64>{}, Int<2>{}, Int<K32>{});
+        if (cols <= 8192) return fn(Int<64>{}, Int<4>{}, Int<K32>{});
+        if (cols <= 16384) return fn(Int<64>{}, Int<8>{}, Int<K32>{});
+        return fn(Int<64>{}, Int<16>{}, Int<K32>{});
+    }
 }
 
 template <class E, class W>
 spccl_status_t launch_forward(const LnArgs& g, hipStream_t st) {
-    if (g.cols > kMaxCols) {
+    if (g.cols > kMaxCols || g.cols < (uint32_t)E::vec) {
         hipLaunchKernelGGL((k_layer_norm_long<E, W>), dim3((uint32_t)g.rows), dim3(1024), 0, st, g);
         return launch_status();
     }
     with_row<E, false>(g.cols, [&](auto l, auto waves, auto k) {
         using R = Row<E, l(), waves(), k()>;
-        hipLaunchKernelGGL((k_layer_norm<E, W, l(), waves(), k()>), dim3((uint32_t)((g.rows + R::rows - 1) / R::rows)),
-                           dim3(R::threads), 0, st, g);
+        const dim3 grid((uint32_t)((g.rows + R::rows - 1) / R::rows)), block(R::threads);
+        if (g.cols % E::vec) hipLaunchKernelGGL((k_layer_norm<E, W, l(), waves(), k(), true>), grid, block, 0, st, g);
+        else hipLaunchKernelGGL((k_layer_norm<E, W, l(), waves(), k(), false>), grid, block, 0, st, g);
     });
     return launch_status();
 }
 
-// Blocks of a backward pass, each of which leaves two sums per column.
-constexpr uint32_t kBackBlocks = 1024, kStrips = 64;
+// Blocks of a backward pass, each of which leaves two sums per column: one per
+// CU, as every further block's sums are written and read again (65536 x 4096
+// bf16: 268 us; with 512 blocks of 256 threads 277, with 1024 blocks 353).
+constexpr uint32_t kBackBlocks = 256, kStrips = 64;
 uint32_t back_blocks(uint64_t rows, uint32_t rows_per_block) {
     const uint64_t b = (rows + rows_per_block - 1) / rows_per_block;
     return (uint32_t)(b < kBackBlocks ? b : kBackBlocks);
@@ -643,16 +802,16 @@ uint32_t strips(uint64_t rows) { return (uint32_t)(rows < kStrips ? rows : kStri
 
 template <class E>
 uint32_t back_parts(uint64_t rows, uint32_t cols) {
-    if (cols > kMaxBackCols) return strips(rows);
+    if (cols > kMaxBackCols || cols < (uint32_t)E::vec) return strips(rows);
     return with_row<E, true>(cols, [&](auto l, auto waves, auto k) {
-        return back_blocks(rows, Row<E, l(), waves(), k()>::rows);
+        return back_blocks(rows, Row<E, l(), waves(), k(), kBackThreads>::rows);
     });
 }
 
 template <class E, class W>
 spccl_status_t launch_backward(const LnBackArgs& g, int32_t gdtype, void* dw, void* db, int32_t accumulate,
                                hipStream_t st) {
-    if (g.cols > kMaxBackCols) {
+    if (g.cols > kMaxBackCols || g.cols < (uint32_t)E::vec) {
         // the columns' sums first: dx may be written over dy or x
         if (g.part) {
             hipLaunchKernelGGL(k_layer_norm_columns<E>, dim3((g.cols + 64 * E::vec - 1) / (64 * E::vec), strips(g.rows)),
@@ -662,9 +821,10 @@ spccl_status_t launch_backward(const LnBackArgs& g, int32_t gdtype, void* dw, vo
         if (g.dx) hipLaunchKernelGGL((k_layer_norm_back_long<E, W>), dim3((uint32_t)g.rows), dim3(1024), 0, st, g);
     } else {
         with_row<E, true>(g.cols, [&](auto l, auto waves, auto k) {
-            using R = Row<E, l(), waves(), k()>;
-            hipLaunchKernelGGL((k_layer_norm_back<E, W, l(), waves(), k()>), dim3(back_blocks(g.rows, R::rows)),
-                               dim3(R::threads), 0, st, g);
+            using R = Row<E, l(), waves(), k(), kBackThreads>;
+            const dim3 grid(back_blocks(g.rows, R::rows)), block(R::threads);
+            if (g.cols % E::vec) hipLaunchKernelGGL((k_layer_norm_back<E, W, l(), waves(), k(), true>), grid, block, 0, st, g);
+            else hipLaunchKernelGGL((k_layer_norm_back<E, W, l(), waves(), k(), false>), grid, block, 0, st, g);
         });
     }
     if (launch_status() != SPCCL_OK) return SPCCL_ERR_HIP;
@@ -714,8 +874,8 @@ spccl_status_t spccl_layer_norm(const void* x, uint64_t ldx, const void* weight,
 
 uint64_t spccl_layer_norm_scratch_bytes(uint64_t rows, uint64_t cols) {
     if (rows == 0 || rows >= (1ull << 31) || cols == 0 || cols >= (1ull << 31)) return 0;
-    // an fp32 row and a bf16 row of as many columns lie alike over the lanes
-    return 8ull * cols * back_parts<F32>(rows, (uint32_t)cols);
+    const uint32_t a = back_parts<F32>(rows, (uint32_t)cols), b = back_parts<BF16>(rows, (uint32_t)cols);
+    return 8ull * cols * (a > b ? a : b);
 }
 
 spccl_status_t spccl_layer_norm_backward(const void* dy, uint64_t lddy, const void* x, uint64_t ldx, const void* weight,
