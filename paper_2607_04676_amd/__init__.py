@@ -177,9 +177,16 @@ def _dt(t: torch.Tensor) -> int:
     raise TypeError(f"unsupported dtype {t.dtype}")
 
 
+# the current stream's handle without a Stream object (0.1 us against 2.8)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream(stream) -> int:
-    s = stream if stream is not None else torch.cuda.current_stream()
-    return s.cuda_stream
+    if stream is not None:
+        return stream.cuda_stream
+    if _raw_stream is not None:
+        return _raw_stream(torch.cuda.current_device())
+    return torch.cuda.current_stream().cuda_stream
 
 
 def _nbytes(t: torch.Tensor) -> int:
@@ -466,28 +473,31 @@ def alloc_sliced(n: int, dtype: int, device="cuda") -> torch.Tensor:
 
 # ---- layer norm ---------------------------------------------------------------------
 
-def _matrix(t: torch.Tensor, like: torch.Tensor | None, what: str) -> int:
+def _matrix(t: torch.Tensor, like: torch.Tensor, what: str) -> int:
     """The row pitch of a matrix whose rows are contiguous, of the same shape
     and dtype as `like`."""
-    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
-        raise ValueError(f"{what}: a matrix with contiguous rows is needed, got shape {tuple(t.shape)} strides {t.stride()}")
-    if like is not None and (t.shape != like.shape or t.dtype != like.dtype):
+    if t is not like and (t.shape != like.shape or t.dtype != like.dtype):
         raise ValueError(f"{what}: {tuple(t.shape)} {t.dtype} does not match {tuple(like.shape)} {like.dtype}")
-    return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 1)
+    strides = t.stride()
+    if len(strides) != 2 or (strides[1] != 1 and t.shape[1] > 1):
+        raise ValueError(f"{what}: a matrix with contiguous rows is needed, got shape {tuple(t.shape)} strides {strides}")
+    return strides[0] if t.shape[0] > 1 else max(t.shape[1], 1)
 
 
-def _vector(t: torch.Tensor | None, n: int, what: str, dtype=None) -> None:
-    if t is not None and (t.dim() != 1 or t.numel() != n or not (t.is_contiguous())
-                          or (dtype is not None and t.dtype != dtype)):
-        raise ValueError(f"{what}: {n} contiguous elements{f' of {dtype}' if dtype else ''} are needed, got "
-                         f"shape {tuple(t.shape)} {t.dtype}")
+def _vector(t: torch.Tensor, n: int, what: str, dtype) -> int:
+    """The address of n contiguous elements of a dtype."""
+    if t.shape != (n,) or t.dtype != dtype or not t.is_contiguous():
+        raise ValueError(f"{what}: {n} contiguous elements of {dtype} are needed, got shape {tuple(t.shape)} {t.dtype}")
+    return t.data_ptr()
 
 
-def _dt_of_pair(a, b, otherwise: int, what: str) -> int:
-    given = [t for t in (a, b) if t is not None]
-    if len({t.dtype for t in given}) > 1:
-        raise ValueError(f"{what}: {given[0].dtype} and {given[1].dtype}")
-    return _dt(given[0]) if given else otherwise
+def _vectors(a: torch.Tensor | None, b: torch.Tensor | None, n: int, what: str, otherwise: int) -> tuple:
+    """Addresses of two vectors of one dtype (either may be None), and the dtype."""
+    if a is None and b is None:
+        return None, None, otherwise
+    dtype = (b if a is None else a).dtype
+    return (None if a is None else _vector(a, n, what, dtype), None if b is None else _vector(b, n, what, dtype),
+            _dt(b if a is None else a))
 
 
 def spccl_layer_norm(x: torch.Tensor, weight: torch.Tensor | None, bias: torch.Tensor | None, y: torch.Tensor,
@@ -495,15 +505,13 @@ def spccl_layer_norm(x: torch.Tensor, weight: torch.Tensor | None, bias: torch.T
                      stream=None) -> None:
     """y = layer norm of x's rows; mean and rstd (fp32, one per row) are written
     for the backward pass."""
-    ldx, ldy = _matrix(x, None, "x"), _matrix(y, x, "y")
+    ldx, ldy = _matrix(x, x, "x"), _matrix(y, x, "y")
     rows, cols = x.shape
-    for t, n, what, dt in ((weight, cols, "weight", None), (bias, cols, "bias", None),
-                           (mean, rows, "mean", torch.float32), (rstd, rows, "rstd", torch.float32)):
-        _vector(t, n, what, dt)
-    _check(_lib.spccl_layer_norm(x.data_ptr(), ldx, _ptr_or_null(weight), _ptr_or_null(bias), y.data_ptr(), ldy,
-                                 _ptr_or_null(mean), _ptr_or_null(rstd), rows, cols, _dt(x),
-                                 _dt_of_pair(weight, bias, _dt(x), "weight and bias"), float(eps), _stream(stream)),
-           "spccl_layer_norm")
+    w, b, wdt = _vectors(weight, bias, cols, "weight and bias", SPCCL_F32)
+    m = None if mean is None else _vector(mean, rows, "mean", torch.float32)
+    r = None if rstd is None else _vector(rstd, rows, "rstd", torch.float32)
+    _check(_lib.spccl_layer_norm(x.data_ptr(), ldx, w, b, y.data_ptr(), ldy, m, r, rows, cols, _dt(x), wdt, eps,
+                                 _stream(stream)), "spccl_layer_norm")
 
 
 def spccl_layer_norm_scratch_bytes(rows: int, cols: int) -> int:
@@ -516,17 +524,14 @@ def spccl_layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: torch.T
                               accumulate: bool = False, stream=None) -> None:
     """The gradients of sum(dy * y): dx, and the weight's and the bias's (any
     None: not wanted), added to what they hold if `accumulate`."""
-    ldx, lddy = _matrix(x, None, "x"), _matrix(dy, x, "dy")
+    ldx, lddy = _matrix(x, x, "x"), _matrix(dy, x, "dy")
     lddx = 0 if dx is None else _matrix(dx, x, "dx")
     rows, cols = x.shape
-    for t, n, what, dt in ((weight, cols, "weight", None), (dweight, cols, "dweight", None),
-                           (dbias, cols, "dbias", None), (mean, rows, "mean", torch.float32),
-                           (rstd, rows, "rstd", torch.float32)):
-        _vector(t, n, what, dt)
+    w, _, wdt = _vectors(weight, None, cols, "weight", SPCCL_F32)
+    dw, db, gdt = _vectors(dweight, dbias, cols, "dweight and dbias", SPCCL_F32)
     _check(_lib.spccl_layer_norm_backward(
-        dy.data_ptr(), lddy, x.data_ptr(), ldx, _ptr_or_null(weight), mean.data_ptr(), rstd.data_ptr(),
-        _ptr_or_null(dx), lddx, _ptr_or_null(dweight), _ptr_or_null(dbias), rows, cols, _dt(x),
-        _dt(x) if weight is None else _dt(weight), _dt_of_pair(dweight, dbias, SPCCL_F32, "dweight and dbias"),
+        dy.data_ptr(), lddy, x.data_ptr(), ldx, w, _vector(mean, rows, "mean", torch.float32),
+        _vector(rstd, rows, "rstd", torch.float32), _ptr_or_null(dx), lddx, dw, db, rows, cols, _dt(x), wdt, gdt,
         1 if accumulate else 0, _ptr_or_null(scratch), 0 if scratch is None else _nbytes(scratch), _stream(stream)),
         "spccl_layer_norm_backward")
 

@@ -132,7 +132,7 @@ struct Place {
         if constexpr (Ragged) {
             a = c + E::vec <= cols ? c : cols - E::vec;
             first = c + E::vec <= cols ? 0 : (c >= cols ? E::vec : c + E::vec - cols);
-            asm("" : "+v"(first));         // masks of its values are made where they are used, not kept
+            asm volatile("" : "+v"(first));         // masks of its values are made where they are used, not kept
         } else {
             a = c < cols ? c : cols - E::vec;
             first = c < cols ? 0 : E::vec;
@@ -607,17 +607,17 @@ __global__ void __launch_bounds__((Row<E, L, Waves, K, kBackThreads>::threads)) 
     }
 }
 
-// Long or very short rows: dx of one row per block, reading the row twice.
-template <class E, class W>
-__global__ void __launch_bounds__(1024) k_layer_norm_back_long(LnBackArgs g) {
+// dx of one row by a whole block, reading the row twice.
+template <class E, class W, uint32_t Threads>
+__device__ __forceinline__ void back_row(const LnBackArgs& g, uint64_t row) {
     constexpr int V = E::vec;
-    __shared__ float s_part[2][16];
-    const uint64_t row = blockIdx.x;
+    constexpr uint32_t waves = Threads / 64;
+    __shared__ float s_part[2][waves];
     const uint8_t* px = g.x + row * g.ldx;
     const uint8_t* pdy = g.dy + row * g.lddy;
     const float mean = g.mean[row], rstd = g.rstd[row];
     float s1 = 0.f, s2 = 0.f;
-    for (uint32_t c = threadIdx.x * V; c < g.cols; c += 1024 * V) {
+    for (uint32_t c = threadIdx.x * V; c < g.cols; c += Threads * V) {
         const uint32_t rem = g.cols - c;
         const u32x4 x = load_vec<E>(px, c, rem), dy = load_vec<E>(pdy, c, rem);
         float w[V];
@@ -638,14 +638,14 @@ __global__ void __launch_bounds__(1024) k_layer_norm_back_long(LnBackArgs g) {
     __syncthreads();
     s1 = s2 = 0.f;
 #pragma unroll
-    for (int q = 0; q < 16; q++) {
+    for (uint32_t q = 0; q < waves; q++) {
         s1 += s_part[0][q];
         s2 += s_part[1][q];
     }
     s1 /= (float)g.cols;
     s2 /= (float)g.cols;
     uint8_t* dst = g.dx + row * g.lddx;
-    for (uint32_t c = threadIdx.x * V; c < g.cols; c += 1024 * V) {
+    for (uint32_t c = threadIdx.x * V; c < g.cols; c += Threads * V) {
         const uint32_t rem = g.cols - c;
         const u32x4 x = load_vec<E>(px, c, rem), dy = load_vec<E>(pdy, c, rem);
         float w[V], o[V];
@@ -655,6 +655,67 @@ __global__ void __launch_bounds__(1024) k_layer_norm_back_long(LnBackArgs g) {
             o[j] = fmaf(-((E::get(x, j) - mean) * rstd), s1, fmaf(E::get(dy, j), w[j], -s2)) * rstd;
         store_vec<E>(dst, c, rem, o);
     }
+}
+
+// Long or very short rows.
+template <class E, class W>
+__global__ void __launch_bounds__(1024) k_layer_norm_back_long(LnBackArgs g) {
+    back_row<E, W, 1024>(g, blockIdx.x);
+}
+
+// A small backward pass in one launch: the first `column_blocks` blocks take
+// 256 columns each and add up all rows (8 waves every 8th row, then their
+// sums in order), the others write a row of dx each.  Every element is read
+// twice, from the caches.  In place, dx would be written over what a column
+// block has yet to read: then the two kinds of blocks are two launches
+// (first_block picks them), with the same bits.
+struct LnSmallArgs {
+    uint32_t column_blocks, first_block;
+    void* dw;
+    void* db;
+    int accumulate;
+};
+constexpr uint32_t kSmallThreads = 512;
+template <class E, class W, class G>
+__global__ void __launch_bounds__(kSmallThreads) k_layer_norm_back_small(LnBackArgs g, LnSmallArgs o) {
+    const uint32_t block = blockIdx.x + o.first_block;
+    if (block >= o.column_blocks) {
+        back_row<E, W, kSmallThreads>(g, block - o.column_blocks);
+        return;
+    }
+    constexpr uint32_t waves = kSmallThreads / 64;
+    __shared__ float s_sum[2][waves][256];
+    const uint32_t wave = threadIdx.x >> 6, lane = threadIdx.x & 63u;
+    const uint32_t c = block * 256 + lane * 4;
+    const uint32_t rem = c < g.cols ? (g.cols - c < 4 ? g.cols - c : 4) : 0;
+    float dw[4] = {0.f, 0.f, 0.f, 0.f}, db[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (uint32_t row = wave; row < (uint32_t)g.rows; row += waves) {
+        float x[4], dy[4];
+        load_param<E, 4>(g.x + row * g.ldx, c, rem, 0.f, x);
+        load_param<E, 4>(g.dy + row * g.lddy, c, rem, 0.f, dy);
+        const float mean = g.mean[row], rstd = g.rstd[row];
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+            dw[j] = fmaf(dy[j], (x[j] - mean) * rstd, dw[j]);
+            db[j] += dy[j];
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < 4; j++) {
+        s_sum[0][wave][lane * 4 + j] = dw[j];
+        s_sum[1][wave][lane * 4 + j] = db[j];
+    }
+    __syncthreads();
+    const uint32_t which = threadIdx.x >> 8, col = threadIdx.x & 255u;
+    typename G::raw* out = static_cast<typename G::raw*>(which ? o.db : o.dw);
+    const uint32_t at = block * 256 + col;
+    if (!out || at >= g.cols) return;
+    float t = 0.f;
+#pragma unroll
+    for (uint32_t q = 0; q < waves; q++) t += s_sum[which][q][col];
+    if (o.accumulate) t += G::one(out[at]);
+    out[at] = G::round(t);
 }
 
 // Sums of dy h and dy over a strip of rows (grid y), a vector of columns per
@@ -808,9 +869,36 @@ uint32_t back_parts(uint64_t rows, uint32_t cols) {
     });
 }
 
+// Backward passes of so few rows take one launch, k_layer_norm_back_small, at
+// any width (us with the host's part, small / otherwise, bf16: 64 x 1024 9.7 /
+// 12.9, 128 x 8192 9.6 / 16.1, 128 x 131072 46 / 105; with 256 rows 13.3 / 12.8
+// at 1024 columns and 24 / 20 at 8192).
+constexpr uint64_t kSmallRows = 128;
+
+template <class E, class W>
+spccl_status_t launch_small(const LnBackArgs& g, int32_t gdtype, void* dw, void* db, int32_t accumulate, bool in_place,
+                            hipStream_t st) {
+    LnSmallArgs o{g.part ? (g.cols + 255) / 256 : 0, 0, dw, db, accumulate};
+    const uint32_t rows = g.dx ? (uint32_t)g.rows : 0;
+    const auto go = [&](uint32_t first, uint32_t count) {
+        if (!count) return SPCCL_OK;
+        o.first_block = first;
+        if (gdtype == kBF16)
+            hipLaunchKernelGGL((k_layer_norm_back_small<E, W, BF16>), dim3(count), dim3(kSmallThreads), 0, st, g, o);
+        else
+            hipLaunchKernelGGL((k_layer_norm_back_small<E, W, F32>), dim3(count), dim3(kSmallThreads), 0, st, g, o);
+        return launch_status();
+    };
+    if (!in_place) return go(0, o.column_blocks + rows);
+    const spccl_status_t st1 = go(0, o.column_blocks);
+    return st1 == SPCCL_OK ? go(o.column_blocks, rows) : st1;
+}
+
 template <class E, class W>
 spccl_status_t launch_backward(const LnBackArgs& g, int32_t gdtype, void* dw, void* db, int32_t accumulate,
                                hipStream_t st) {
+    if (g.rows <= kSmallRows)
+        return launch_small<E, W>(g, gdtype, dw, db, accumulate, g.dx && (g.dx == g.x || g.dx == g.dy), st);
     if (g.cols > kMaxBackCols || g.cols < (uint32_t)E::vec) {
         // the columns' sums first: dx may be written over dy or x
         if (g.part) {
