@@ -474,8 +474,8 @@ spccl_status_t spccl_vr_all_reduce_sliced(void* const* send, void* const* recv, 
 /* ---- layer norm (a layer of the models whose gradients the collectives reduce) -- */
 
 /* y = (x - mean) * rstd * weight + bias over each row of a matrix of `rows`
- * rows and `cols` columns (cols >= 1, both < 2^31), mean and 1 / sqrt(variance
- * + eps) taken over the row (the biased variance).  ldx, ldy: elements between
+ * rows and `cols` columns (rows < 2^31, 1 <= cols < 2^27), mean and
+ * 1 / sqrt(variance + eps) taken over the row (the biased variance).  ldx, ldy: elements between
  * rows (>= cols).  x and y have `dtype`, weight and bias (NULL: ones, zeros)
  * `wdtype`; sums are held in fp32 and y is rounded once.  mean and rstd
  * (fp32, `rows` each, NULL: not wanted) are what the backward pass reads.
@@ -507,7 +507,7 @@ spccl_status_t spccl_layer_norm_backward(const void* dy, uint64_t lddy, const vo
 /* ---- pruning with error feedback (Sec. VI-B) --------------------------------- */
 
 /* Splits a gradient and its residual by magnitude, for each of n elements
- * (n < 2^40):
+ * (n < 2^36):
  *   a = grad + leak * residual         (fp32, each operation rounded)
  *   out = a rounded to dtype where |a| >= *threshold, +0.0 elsewhere
  *   residual = a - out

@@ -462,7 +462,7 @@ __global__ void __launch_bounds__((Row<E, L, Waves, K, kBackThreads>::threads)) 
     using R = Row<E, L, Waves, K, kBackThreads>;
     using At = Place<E, Ragged>;
     constexpr int V = E::vec;
-    __shared__ float s_sum[R::rows > 1 ? R::cap : 1];
+    __shared__ __attribute__((aligned(16))) float s_sum[R::rows > 1 ? R::rows * R::cap : 1];
     __shared__ float s_row[2][2][R::waves];
     const uint32_t i = threadIdx.x % R::lanes;
     const uint32_t group = R::group();
@@ -497,7 +497,7 @@ __global__ void __launch_bounds__((Row<E, L, Waves, K, kBackThreads>::threads)) 
     };
     // the next row is on its way while this one is worked on, where the
     // registers for it are there (1024 threads have 128 each)
-    constexpr bool Ahead = R::threads <= 512 || K <= 2;
+    constexpr bool Ahead = (R::threads <= 512 && K * V <= 24) || K <= 2;
     const uint64_t step = (uint64_t)gridDim.x * R::rows;
     uint32_t turn = 0;
     Data next;
@@ -571,38 +571,36 @@ __global__ void __launch_bounds__((Row<E, L, Waves, K, kBackThreads>::threads)) 
     }
     if (!g.part) return;
     float* part = g.part + (uint64_t)blockIdx.x * 2 * g.cols;
+    if constexpr (R::rows == 1) {
+#pragma unroll
+        for (int k = 0; k < K; k++) {
+            const At at((k * R::lanes + i) * V, g.cols);
+#pragma unroll
+            for (int j = 0; j < V; j++)
+                if ((uint32_t)j >= at.first) {
+                    part[at.a + j] = dw[k][j];
+                    part[g.cols + at.a + j] = db[k][j];
+                }
+        }
+        return;
+    }
+    // every group leaves its sums in LDS, then each thread adds up columns
 #pragma unroll
     for (int which = 0; which < 2; which++) {
-        float(&acc)[K][V] = which ? db : dw;
-        if constexpr (R::rows > 1) {
-            // a place per lane and element, the same for every group
-            for (uint32_t q = 0; q < R::rows; q++) {
-                __syncthreads();
-                if (group != q) continue;
+        __syncthreads();
 #pragma unroll
-                for (int k = 0; k < K; k++)
+        for (int k = 0; k < K; k++) {
+            const At at((k * R::lanes + i) * V, g.cols);
 #pragma unroll
-                    for (int j = 0; j < V; j++) {
-                        float& sum = s_sum[(k * V + j) * R::lanes + i];
-                        sum = q ? sum + acc[k][j] : acc[k][j];
-                    }
-            }
-            __syncthreads();
-            if (group == 0) {
-#pragma unroll
-                for (int k = 0; k < K; k++)
-#pragma unroll
-                    for (int j = 0; j < V; j++) acc[k][j] = s_sum[(k * V + j) * R::lanes + i];
-            }
+            for (int j = 0; j < V; j++)
+                if ((uint32_t)j >= at.first) s_sum[group * R::cap + at.a + j] = which ? db[k][j] : dw[k][j];
         }
-        if (group == 0) {
-#pragma unroll
-            for (int k = 0; k < K; k++) {
-                const At at((k * R::lanes + i) * V, g.cols);
-#pragma unroll
-                for (int j = 0; j < V; j++)
-                    if ((uint32_t)j >= at.first) part[which * g.cols + at.a + j] = acc[k][j];
-            }
+        __syncthreads();
+        for (uint32_t c = threadIdx.x; c < g.cols; c += R::threads) {
+            float t = 0.f;
+#pragma unroll 8
+            for (uint32_t q = 0; q < R::rows; q++) t += s_sum[q * R::cap + c];
+            part[which * g.cols + c] = t;
         }
     }
 }
@@ -748,9 +746,11 @@ __global__ void __launch_bounds__(64) k_layer_norm_columns(LnBackArgs g) {
         }
 }
 
-// The weight's and the bias's gradient: the sums of `parts` blocks, in their
-// order (16 waves take every 16th each, then one adds the 16), onto what is
-// there where they accumulate.
+// The weight's and the bias's gradient: the sums of `parts` blocks (at most
+// kBackBlocks), 16 waves taking every 16th each with all their loads in
+// flight, then the waves' sums in order, onto what is there where they
+// accumulate.
+constexpr uint32_t kBackBlocks = 256;
 template <class G>
 __global__ void __launch_bounds__(1024) k_layer_norm_grads(const float* part, uint32_t parts, uint32_t cols,
                                                            typename G::raw* dw, typename G::raw* db, int accumulate) {
@@ -758,9 +758,16 @@ __global__ void __launch_bounds__(1024) k_layer_norm_grads(const float* part, ui
     const uint32_t wave = threadIdx.x >> 6, l = threadIdx.x & 63u;
     const uint64_t c = (uint64_t)blockIdx.x * 64 + l;             // column of [dw | db]
     const uint64_t width = 2ull * cols;
+    const float* p = part + (c < width ? c : width - 1);
+    float v[kBackBlocks / 16];
+#pragma unroll
+    for (uint32_t u = 0; u < kBackBlocks / 16; u++) {
+        const uint32_t q = wave + 16 * u;
+        v[u] = p[(uint64_t)(q < parts ? q : 0) * width];
+    }
     float sum = 0.f;
-    if (c < width)
-        for (uint32_t p = wave; p < parts; p += 16) sum += part[p * width + c];
+#pragma unroll
+    for (uint32_t u = 0; u < kBackBlocks / 16; u++) sum += wave + 16 * u < parts ? v[u] : 0.f;
     s_sum[wave][l] = sum;
     __syncthreads();
     if (wave || c >= width) return;
@@ -772,6 +779,15 @@ __global__ void __launch_bounds__(1024) k_layer_norm_grads(const float* part, ui
     const uint64_t at = c < cols ? c : c - cols;
     if (accumulate) t += G::one(out[at]);
     out[at] = G::round(t);
+}
+
+// No rows: the sums are zero.
+template <class G>
+__global__ void __launch_bounds__(256) k_layer_norm_no_grads(uint32_t cols, typename G::raw* dw, typename G::raw* db) {
+    const uint64_t c = (uint64_t)blockIdx.x * 256 + threadIdx.x;
+    if (c >= cols) return;
+    if (dw) dw[c] = G::round(0.f);
+    if (db) db[c] = G::round(0.f);
 }
 
 // ---------------------------------------------------------------------------
@@ -808,7 +824,8 @@ bool span_overlap(const void* p, uint64_t pn, const Rows& m, uint64_t rows, uint
 // columns on a wave's own row takes 16, then 32 (16384 x 1600 bf16: 16.5 us,
 // 17.3 with two waves of 16; 16384 x 1024: 13.8 and 11.3).  The backward pass
 // holds two sums for each element, so its rows take 16 and spread over waves
-// sooner (32: 65536 x 1024 88 us against 74, 65536 x 4096 283 against 268).
+// sooner (32: 65536 x 1024 88 us against 74, 65536 x 4096 283 against 268), 24
+// up to 12288 columns (8192 x 12288: 117 us; 124 with 16 waves of 16).
 constexpr uint32_t kMaxCols = 32768, kMaxBackCols = 16384;       // beyond: the long forms
 
 template <int N>
@@ -826,6 +843,7 @@ auto with_row(uint32_t cols, Fn fn) {
         if (cols <= 2048) return fn(Int<64>{}, Int<2>{}, Int<K16>{});
         if (cols <= 4096) return fn(Int<64>{}, Int<4>{}, Int<K16>{});
         if (cols <= 8192) return fn(Int<64>{}, Int<8>{}, Int<K16>{});
+        if (cols <= 12288) return fn(Int<64>{}, Int<8>{}, Int<24 / E::vec>{});
         return fn(Int<64>{}, Int<16>{}, Int<K16>{});
     } else {
         if (cols <= 2048) return fn(Int<64>{}, Int<1>{}, Int<K32>{});
@@ -836,27 +854,61 @@ auto with_row(uint32_t cols, Fn fn) {
     }
 }
 
+// Launches fn(first, count) over rows, as many at a time as one grid may have
+// threads for (2^32).
+template <class Fn>
+spccl_status_t by_rows(uint64_t rows, uint32_t rows_per_block, uint32_t threads, Fn fn) {
+    const uint64_t most = (uint64_t)(0xFFFFFFFFu / threads) * rows_per_block;
+    for (uint64_t first = 0; first < rows; first += most) {
+        fn(first, rows - first < most ? rows - first : most);
+        if (launch_status() != SPCCL_OK) return SPCCL_ERR_HIP;
+    }
+    return SPCCL_OK;
+}
+
+LnArgs rows_of(LnArgs g, uint64_t first, uint64_t count) {
+    g.x += first * g.ldx;
+    g.y += first * g.ldy;
+    if (g.mean) g.mean += first;
+    if (g.rstd) g.rstd += first;
+    g.rows = count;
+    return g;
+}
+LnBackArgs rows_of(LnBackArgs g, uint64_t first, uint64_t count) {
+    g.x += first * g.ldx;
+    g.dy += first * g.lddy;
+    g.dx += first * g.lddx;
+    g.mean += first;
+    g.rstd += first;
+    g.rows = count;
+    return g;
+}
+
 template <class E, class W>
 spccl_status_t launch_forward(const LnArgs& g, hipStream_t st) {
-    if (g.cols > kMaxCols || g.cols < (uint32_t)E::vec) {
-        hipLaunchKernelGGL((k_layer_norm_long<E, W>), dim3((uint32_t)g.rows), dim3(1024), 0, st, g);
-        return launch_status();
-    }
-    with_row<E, false>(g.cols, [&](auto l, auto waves, auto k) {
+    if (g.cols > kMaxCols || g.cols < (uint32_t)E::vec)
+        return by_rows(g.rows, 1, 1024, [&](uint64_t first, uint64_t count) {
+            hipLaunchKernelGGL((k_layer_norm_long<E, W>), dim3((uint32_t)count), dim3(1024), 0, st, rows_of(g, first, count));
+        });
+    return with_row<E, false>(g.cols, [&](auto l, auto waves, auto k) {
         using R = Row<E, l(), waves(), k()>;
-        const dim3 grid((uint32_t)((g.rows + R::rows - 1) / R::rows)), block(R::threads);
-        if (g.cols % E::vec) hipLaunchKernelGGL((k_layer_norm<E, W, l(), waves(), k(), true>), grid, block, 0, st, g);
-        else hipLaunchKernelGGL((k_layer_norm<E, W, l(), waves(), k(), false>), grid, block, 0, st, g);
+        return by_rows(g.rows, R::rows, R::threads, [&](uint64_t first, uint64_t count) {
+            const dim3 grid((uint32_t)((count + R::rows - 1) / R::rows)), block(R::threads);
+            const LnArgs part = rows_of(g, first, count);
+            if (g.cols % E::vec) hipLaunchKernelGGL((k_layer_norm<E, W, l(), waves(), k(), true>), grid, block, 0, st, part);
+            else hipLaunchKernelGGL((k_layer_norm<E, W, l(), waves(), k(), false>), grid, block, 0, st, part);
+        });
     });
-    return launch_status();
 }
 
 // Blocks of a backward pass, each of which leaves two sums per column: one per
 // CU, as every further block's sums are written and read again (65536 x 4096
-// bf16: 268 us; with 512 blocks of 256 threads 277, with 1024 blocks 353).
-constexpr uint32_t kBackBlocks = 256, kStrips = 64;
+// bf16: 268 us; with 512 blocks of 256 threads 277, with 1024 blocks 353), and
+// none for less than two rounds of rows (307 x 11622: 25 us; one round 36, four
+// 29).
+constexpr uint32_t kStrips = 64;
 uint32_t back_blocks(uint64_t rows, uint32_t rows_per_block) {
-    const uint64_t b = (rows + rows_per_block - 1) / rows_per_block;
+    const uint64_t b = (rows + 2 * rows_per_block - 1) / (2 * rows_per_block);
     return (uint32_t)(b < kBackBlocks ? b : kBackBlocks);
 }
 uint32_t strips(uint64_t rows) { return (uint32_t)(rows < kStrips ? rows : kStrips); }
@@ -906,7 +958,13 @@ spccl_status_t launch_backward(const LnBackArgs& g, int32_t gdtype, void* dw, vo
                                dim3(64), 0, st, g);
             if (launch_status() != SPCCL_OK) return SPCCL_ERR_HIP;
         }
-        if (g.dx) hipLaunchKernelGGL((k_layer_norm_back_long<E, W>), dim3((uint32_t)g.rows), dim3(1024), 0, st, g);
+        if (g.dx) {
+            const spccl_status_t st1 = by_rows(g.rows, 1, 1024, [&](uint64_t first, uint64_t count) {
+                hipLaunchKernelGGL((k_layer_norm_back_long<E, W>), dim3((uint32_t)count), dim3(1024), 0, st,
+                                   rows_of(g, first, count));
+            });
+            if (st1 != SPCCL_OK) return st1;
+        }
     } else {
         with_row<E, true>(g.cols, [&](auto l, auto waves, auto k) {
             using R = Row<E, l(), waves(), k(), kBackThreads>;
@@ -939,7 +997,7 @@ spccl_status_t spccl_layer_norm(const void* x, uint64_t ldx, const void* weight,
                                 float* mean, float* rstd, uint64_t rows, uint64_t cols, int32_t dtype, int32_t wdtype,
                                 double eps, void* stream) {
     if (!dtype_ok(dtype) || !dtype_ok(wdtype)) return SPCCL_ERR_UNSUPPORTED;
-    if (rows >= (1ull << 31) || cols >= (1ull << 31)) return SPCCL_ERR_UNSUPPORTED;
+    if (rows >= (1ull << 31) || cols >= (1ull << 27)) return SPCCL_ERR_UNSUPPORTED;
     if (cols == 0 || ldx < cols || ldy < cols || !(eps >= 0.0)) return SPCCL_ERR_INVALID_ARG;
     if (rows == 0) return SPCCL_OK;
     if (!x || !y || !aligned(x, dtype) || !aligned(y, dtype) || !aligned(weight, wdtype) || !aligned(bias, wdtype) ||
@@ -961,7 +1019,7 @@ spccl_status_t spccl_layer_norm(const void* x, uint64_t ldx, const void* weight,
 }
 
 uint64_t spccl_layer_norm_scratch_bytes(uint64_t rows, uint64_t cols) {
-    if (rows == 0 || rows >= (1ull << 31) || cols == 0 || cols >= (1ull << 31)) return 0;
+    if (rows == 0 || rows >= (1ull << 31) || cols == 0 || cols >= (1ull << 27)) return 0;
     const uint32_t a = back_parts<F32>(rows, (uint32_t)cols), b = back_parts<BF16>(rows, (uint32_t)cols);
     return 8ull * cols * (a > b ? a : b);
 }
@@ -972,7 +1030,7 @@ spccl_status_t spccl_layer_norm_backward(const void* dy, uint64_t lddy, const vo
                                          int32_t gdtype, int32_t accumulate, void* scratch, uint64_t scratch_bytes,
                                          void* stream) {
     if (!dtype_ok(dtype) || !dtype_ok(wdtype) || !dtype_ok(gdtype)) return SPCCL_ERR_UNSUPPORTED;
-    if (rows >= (1ull << 31) || cols >= (1ull << 31)) return SPCCL_ERR_UNSUPPORTED;
+    if (rows >= (1ull << 31) || cols >= (1ull << 27)) return SPCCL_ERR_UNSUPPORTED;
     if (cols == 0 || lddy < cols || ldx < cols || (dx && lddx < cols)) return SPCCL_ERR_INVALID_ARG;
     if (!aligned(dweight, gdtype) || !aligned(dbias, gdtype)) return SPCCL_ERR_INVALID_ARG;
     const bool grads = dweight || dbias;
@@ -1009,13 +1067,13 @@ spccl_status_t spccl_layer_norm_backward(const void* dy, uint64_t lddy, const vo
     if (rows == 0) {
         // no rows: the sums are zero
         if (!grads || accumulate) return SPCCL_OK;
-        const dim3 grid((uint32_t)((2 * cols + 63) / 64)), block(1024);
+        const dim3 grid((uint32_t)((cols + 255) / 256)), block(256);
         if (gdtype == kBF16)
-            hipLaunchKernelGGL(k_layer_norm_grads<BF16>, grid, block, 0, st, static_cast<const float*>(nullptr), 0u,
-                               (uint32_t)cols, static_cast<uint16_t*>(dweight), static_cast<uint16_t*>(dbias), 0);
+            hipLaunchKernelGGL(k_layer_norm_no_grads<BF16>, grid, block, 0, st, (uint32_t)cols,
+                               static_cast<uint16_t*>(dweight), static_cast<uint16_t*>(dbias));
         else
-            hipLaunchKernelGGL(k_layer_norm_grads<F32>, grid, block, 0, st, static_cast<const float*>(nullptr), 0u,
-                               (uint32_t)cols, static_cast<uint32_t*>(dweight), static_cast<uint32_t*>(dbias), 0);
+            hipLaunchKernelGGL(k_layer_norm_no_grads<F32>, grid, block, 0, st, (uint32_t)cols,
+                               static_cast<uint32_t*>(dweight), static_cast<uint32_t*>(dbias));
         return launch_status();
     }
     if (!dx && !grads) return SPCCL_OK;

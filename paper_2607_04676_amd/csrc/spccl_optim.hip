@@ -8,8 +8,9 @@
 //           p = p (1 - lr wd) - lr / (1 - b1^t) m / (sqrt(v) / sqrt(1 - b2^t) + eps)
 //
 // Both are bound by memory: every array is read and written once and nothing is
-// kept for a second pass.  All arithmetic is fp32, each operation rounded by itself (no
-// contraction), so equal inputs give equal bits wherever it is computed.
+// kept for a second pass.  All arithmetic is fp32, each operation rounded by
+// itself (no contraction), so equal inputs give equal bits wherever it is
+// computed.
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -637,16 +638,15 @@ spccl_status_t check_spans(const spccl_adamw_tensor_t* t, int32_t count, int32_t
 
 template <int PT, int GT, bool Eight>
 spccl_status_t launch_adamw(const spccl_adamw_plan_t& plan, AdamArgs a, hipStream_t st) {
-    if (plan.array_chunks) {
-        a.chunk0 = 0;
-        hipLaunchKernelGGL((k_adamw<PT, GT, Eight, false>), dim3((uint32_t)plan.array_chunks), dim3(kThreads), 0, st, a);
-        if (launch_status() != SPCCL_OK) return SPCCL_ERR_HIP;
-    }
-    if (plan.stream_chunks) {
-        a.chunk0 = plan.array_chunks;
-        hipLaunchKernelGGL((k_adamw<PT, GT, Eight, true>), dim3((uint32_t)plan.stream_chunks), dim3(kThreads), 0, st, a);
-        if (launch_status() != SPCCL_OK) return SPCCL_ERR_HIP;
-    }
+    constexpr uint64_t most = 0xFFFFFFFFu / kThreads;            // a grid has fewer than 2^32 threads
+    const uint64_t ends[2] = {plan.array_chunks, plan.array_chunks + plan.stream_chunks};
+    for (int stream = 0; stream < 2; stream++)
+        for (a.chunk0 = stream ? ends[0] : 0; a.chunk0 < ends[stream]; a.chunk0 += most) {
+            const dim3 grid((uint32_t)std::min(most, ends[stream] - a.chunk0));
+            if (stream) hipLaunchKernelGGL((k_adamw<PT, GT, Eight, true>), grid, dim3(kThreads), 0, st, a);
+            else hipLaunchKernelGGL((k_adamw<PT, GT, Eight, false>), grid, dim3(kThreads), 0, st, a);
+            if (launch_status() != SPCCL_OK) return SPCCL_ERR_HIP;
+        }
     return SPCCL_OK;
 }
 
@@ -660,7 +660,7 @@ extern "C" {
 spccl_status_t spccl_prune(const void* grad, float* residual, const float* threshold, double leak, void* out, uint64_t n,
                            int32_t dtype, void* stream) {
     if (!dtype_ok(dtype)) return SPCCL_ERR_UNSUPPORTED;
-    if (n >= (1ull << 40)) return SPCCL_ERR_UNSUPPORTED;
+    if (n >= (1ull << 36)) return SPCCL_ERR_UNSUPPORTED;          // a grid has fewer than 2^32 threads
     if (!(leak >= 0.0 && leak <= 1.0)) return SPCCL_ERR_INVALID_ARG;
     if (!threshold || !aligned_to(threshold, 4)) return SPCCL_ERR_INVALID_ARG;
     if (n == 0) return SPCCL_OK;
@@ -696,7 +696,6 @@ spccl_status_t spccl_adamw_plan(const spccl_adamw_tensor_t* tensors, int32_t cou
     }
     uint64_t arrays, streams;
     const uint64_t need = table_bytes(tensors, count, &arrays, &streams);
-    if (arrays >= (1ull << 31) || streams >= (1ull << 31)) return SPCCL_ERR_UNSUPPORTED;
     if (count && (!table || !aligned_to(table, 16))) return SPCCL_ERR_INVALID_ARG;
     if (bytes < need) return SPCCL_ERR_WORKSPACE;
     spccl_status_t st = check_spans(tensors, count, param_dtype, state, table, need);

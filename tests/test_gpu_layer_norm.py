@@ -273,6 +273,30 @@ def test_rows_past_32_bit_offsets(S):
     within(dw, ew, bw + OUT["f32"] * ew.abs(), "dweight")
 
 
+@pytest.mark.parametrize("dtype,cols", [("bf16", 3), ("f32", 2)])
+def test_more_rows_than_one_grid_of_long_rows(S, dtype, cols):
+    """Rows shorter than a vector take a block each: more of them than a grid of
+    such blocks may hold."""
+    log(f"layer norm many short rows {dtype} {cols}")
+    rows = (1 << 22) + 77
+    x, dy = matrix(rows, cols, dtype, 1, 2.0, 0.5), matrix(rows, cols, dtype, 2)
+    y, dx = torch.empty_like(x), torch.empty_like(x)
+    mean, rstd = torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+    S.spccl_layer_norm(x, None, None, y, mean, rstd)
+    dw, db = torch.empty(cols, device="cuda"), torch.empty(cols, device="cuda")
+    scratch, _ = scratch_for(S, rows, cols)
+    S.spccl_layer_norm_backward(dy, x, None, mean, rstd, dx, dw, db, scratch)
+    torch.cuda.synchronize()
+    (m, em), (r, er), (e, ee) = forward_bounds(x, None, None, 1e-5, dtype)
+    within(mean[:, None], m, em, "mean")
+    within(rstd[:, None], r, er, "rstd")
+    within(y, e, ee, "y")
+    (ex, bx), (ew, bw), (eb, bb) = backward_bounds(dy, x, None, mean, rstd, dtype)
+    within(dx, ex, bx, "dx")
+    within(dw, ew, bw + OUT["f32"] * ew.abs(), "dweight")
+    within(db, eb, bb + OUT["f32"] * eb.abs(), "dbias")
+
+
 def test_gradient_against_differences(S):
     """Central differences of the forward kernel along random directions.  The
     step's own error is that of the same differences in 64 bits; the kernel's
