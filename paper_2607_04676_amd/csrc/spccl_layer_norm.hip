@@ -496,8 +496,8 @@ __global__ void __launch_bounds__((Row<E, L, Waves, K, kBackThreads>::threads)) 
         d.rstd = g.rstd[row];
     };
     // the next row is on its way while this one is worked on, where the
-    // registers for it are there (1024 threads have 128 each)
-    constexpr bool Ahead = (R::threads <= 512 && K * V <= 24) || K <= 2;
+    // registers for it are there (not for 32 fp32 elements a lane)
+    constexpr bool Ahead = K <= 6;
     const uint64_t step = (uint64_t)gridDim.x * R::rows;
     uint32_t turn = 0;
     Data next;
@@ -520,6 +520,8 @@ __global__ void __launch_bounds__((Row<E, L, Waves, K, kBackThreads>::threads)) 
         for (int k = 0; k < K; k++) {
             w.pin(k);
             At((k * R::lanes + i) * V, mine ? g.cols : 0).clear(dy[k]);
+            // in place, the last row may already be written over (0 times a NaN is one)
+            if (R::rows > 1) x[k] = mine ? x[k] : u32x4{0, 0, 0, 0};
 #pragma unroll
             for (int j = 0; j < V; j++) {
                 const float d = E::get(dy[k], j);
@@ -824,8 +826,9 @@ bool span_overlap(const void* p, uint64_t pn, const Rows& m, uint64_t rows, uint
 // columns on a wave's own row takes 16, then 32 (16384 x 1600 bf16: 16.5 us,
 // 17.3 with two waves of 16; 16384 x 1024: 13.8 and 11.3).  The backward pass
 // holds two sums for each element, so its rows take 16 and spread over waves
-// sooner (32: 65536 x 1024 88 us against 74, 65536 x 4096 283 against 268), 24
-// up to 12288 columns (8192 x 12288: 117 us; 124 with 16 waves of 16).
+// sooner (32: 65536 x 1024 88 us against 74, 65536 x 4096 283 against 268); from
+// 8193 columns on 8 waves take 24, then 32 (8192 x 12288: 117 us; 124 with 16
+// waves of 16, whose blocks leave a lane 128 registers).
 constexpr uint32_t kMaxCols = 32768, kMaxBackCols = 16384;       // beyond: the long forms
 
 template <int N>
@@ -844,7 +847,7 @@ auto with_row(uint32_t cols, Fn fn) {
         if (cols <= 4096) return fn(Int<64>{}, Int<4>{}, Int<K16>{});
         if (cols <= 8192) return fn(Int<64>{}, Int<8>{}, Int<K16>{});
         if (cols <= 12288) return fn(Int<64>{}, Int<8>{}, Int<24 / E::vec>{});
-        return fn(Int<64>{}, Int<16>{}, Int<K16>{});
+        return fn(Int<64>{}, Int<8>{}, Int<K32>{});
     } else {
         if (cols <= 2048) return fn(Int<64>{}, Int<1>{}, Int<K32>{});
         if (cols <= 4096) return fn(Int<64>{}, Int<2>{}, Int<K32>{});

@@ -234,6 +234,26 @@ def test_backward_of_parts_in_place_and_twice(S, rows, cols):
             assert torch.equal(over, dx) and torch.equal(dw, dw2) and torch.equal(db, db2)
 
 
+@pytest.mark.parametrize("rows,cols", [(133, 64), (133, 63), (261, 1000), (515, 2048), (259, 4096), (300, 12_000), (131, 20_000)])
+@pytest.mark.parametrize("over", ["x", "dy", "apart"])
+def test_a_nan_gradient_stays_in_its_row_and_column(S, rows, cols, over):
+    """A NaN in dy's last row: that row of dx and that column's sums are NaN and
+    nothing else, wherever dx is written and however the rows fill the blocks."""
+    log(f"layer norm backward nan {rows}x{cols} {over}")
+    x, dy = matrix(rows, cols, "f32", 1, 2.0, 0.5), matrix(rows, cols, "f32", 2)
+    mean = x.mean(1)
+    rstd = 1.0 / (x.var(1, unbiased=False) + 1e-5).sqrt()
+    dy[rows - 1, 5] = float("nan")
+    dx = {"x": x, "dy": dy, "apart": torch.empty_like(x)}[over]
+    dw, db = torch.empty(cols, device="cuda"), torch.empty(cols, device="cuda")
+    scratch, _ = scratch_for(S, rows, cols)
+    S.spccl_layer_norm_backward(dy, x, None, mean, rstd, dx, dw, db, scratch)
+    torch.cuda.synchronize()
+    assert bool(dx[:rows - 1].isfinite().all()) and bool(dx[rows - 1].isnan().all())
+    for g in (dw, db):
+        assert g.isnan().nonzero().flatten().tolist() == [5]
+
+
 def test_no_rows(S):
     log("layer norm without rows")
     x = torch.empty((0, 80), device="cuda")
