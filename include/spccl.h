@@ -591,7 +591,8 @@ typedef struct {
  * rounded to 8 bits.  An element that a message leaves out has a gradient of
  * zero.  Element i of tensor k takes its random bits from the seed and from
  * i + the sum over earlier tensors of n rounded up to 64: equal calls give
- * equal bits.  ws: at least the 256-byte control block of a workspace; a
+ * equal bits.  A step captured into a HIP graph replays with the values of
+ * `hyper` at its capture.  ws: at least the 256-byte control block of a workspace; a
  * message that fails its header checks sets SPCCL_ERR_CORRUPT_STREAM there and
  * its tensors are not changed; a tile that fails its checks counts as empty. */
 spccl_status_t spccl_adamw_step(const spccl_adamw_plan_t* plan, const spccl_adamw_t* hyper, const float* grad_scale,

@@ -282,9 +282,9 @@ struct LnArgs {
 // meets one barrier.  A row of one wave reads its weights along with x; a
 // longer one afterwards, as their registers would cost it waves (32768 x 8192
 // bf16: 181 us against 194; 16384 x 1024: 11.3 early, 12.1 late).  Stores
-// are non-temporal, loads are not (10007 x 1600 fp32: 20.4 us; 27.1 with
-// ordinary stores, 25.4 with non-temporal loads too).  65536 x 4096 of either
-// type and 32768 x 8192 bf16 run at 5.9 TB/s.
+// are non-temporal, loads are not (10007 x 1600 fp32: 20.3 us; 27.1 with
+// ordinary stores, 25.4 with non-temporal loads too: 6.3 TB/s; 32768 x 8192 bf16
+// runs at 5.9 TB/s).
 template <class E, class W, int L, int Waves, int K, bool Ragged>
 __global__ void __launch_bounds__((Row<E, L, Waves, K>::threads)) k_layer_norm(LnArgs g) {
     using R = Row<E, L, Waves, K>;
@@ -456,7 +456,7 @@ constexpr uint32_t kBackThreads = 512;
 // dy in registers; a block joins its groups' through LDS, in their order, and
 // leaves one pair of sums per column for k_layer_norm_grads, so no sum depends
 // on which block comes first.  All accesses are non-temporal (65536 x 4096
-// bf16, 1.6 GB: 268 us, 6.0 TB/s; 288 with ordinary loads).
+// bf16, 1.6 GB: 266 us, 6.0 TB/s; 288 with ordinary loads).
 template <class E, class W, int L, int Waves, int K, bool Ragged>
 __global__ void __launch_bounds__((Row<E, L, Waves, K, kBackThreads>::threads)) k_layer_norm_back(LnBackArgs g) {
     using R = Row<E, L, Waves, K, kBackThreads>;
