@@ -254,6 +254,9 @@ struct Row {
     static constexpr uint32_t threads = 64 * Waves > Threads ? 64 * Waves : Threads;
     static constexpr uint32_t rows = threads / lanes;             // rows of a block at a time
     static constexpr uint32_t waves = threads / 64;
+    // whether vector k lies past the row's end in every lane, or in some
+    static __device__ __forceinline__ bool beyond(int k, uint32_t cols) { return k * lanes * E::vec >= cols; }
+    static __device__ __forceinline__ bool edge(int k, uint32_t cols) { return (k + 1) * lanes * E::vec > cols; }
     // the thread's row of the block; whole waves know it as a scalar
     static __device__ __forceinline__ uint32_t group() {
         if constexpr (L == 64) return (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)) / Waves;
@@ -307,10 +310,13 @@ __global__ void __launch_bounds__((Row<E, L, Waves, K>::threads)) k_layer_norm(L
         w.load(g.w, a, 1.f);
         b.load(g.b, a, 0.f);
     }
+    // masks of single elements are worth a branch around them
+    constexpr bool Branch = Ragged && K > 2;
     float sum = 0.f;
 #pragma unroll
     for (int k = 0; k < K; k++) {
-        At((k * R::lanes + i) * V, g.cols).clear(v[k]);
+        if (Branch && R::beyond(k, g.cols)) break;
+        if (!Branch || R::edge(k, g.cols)) At((k * R::lanes + i) * V, g.cols).clear(v[k]);
 #pragma unroll
         for (int j = 0; j < V; j++) sum += E::get(v[k], j);
     }
@@ -328,14 +334,24 @@ __global__ void __launch_bounds__((Row<E, L, Waves, K>::threads)) k_layer_norm(L
     float dev = 0.f;
 #pragma unroll
     for (int k = 0; k < K; k++) {
-        const At at((k * R::lanes + i) * V, g.cols);
+        if (Branch && R::beyond(k, g.cols)) break;
         float part = 0.f;
+        if (!Branch || R::edge(k, g.cols)) {
+            const At at((k * R::lanes + i) * V, g.cols);
 #pragma unroll
-        for (int j = 0; j < V; j++) {
-            const float d = !Ragged || (uint32_t)j >= at.first ? E::get(v[k], j) - mean : 0.f;
-            part = fmaf(d, d, part);
+            for (int j = 0; j < V; j++) {
+                const float d = !Ragged || (uint32_t)j >= at.first ? E::get(v[k], j) - mean : 0.f;
+                part = fmaf(d, d, part);
+            }
+            part = at.any() ? part : 0.f;
+        } else {
+#pragma unroll
+            for (int j = 0; j < V; j++) {
+                const float d = E::get(v[k], j) - mean;
+                part = fmaf(d, d, part);
+            }
         }
-        dev += at.any() ? part : 0.f;
+        dev += part;
     }
     dev = lanes_sum<L>(dev);
     if constexpr (Waves > 1) {
@@ -374,6 +390,7 @@ __global__ void __launch_bounds__((Row<E, L, Waves, K>::threads)) k_layer_norm(L
     }
 #pragma unroll
     for (int k = 0; k < K; k++) {
+        if (Branch && R::beyond(k, g.cols)) break;
         float y[V];
 #pragma unroll
         for (int j = 0; j < V; j++) y[j] = fmaf((E::get(v[k], j) - mean) * rstd, w.get(k, j), b.get(k, j));
@@ -455,8 +472,8 @@ constexpr uint32_t kBackThreads = 512;
 // Each group of lanes walks over rows, keeping its columns' sums of dy h and
 // dy in registers; a block joins its groups' through LDS, in their order, and
 // leaves one pair of sums per column for k_layer_norm_grads, so no sum depends
-// on which block comes first.  All accesses are non-temporal (65536 x 4096
-// bf16, 1.6 GB: 266 us, 6.0 TB/s; 288 with ordinary loads).
+// on which block comes first.  Rows of whole vectors are read non-temporally
+// (65536 x 4096 bf16, 1.6 GB: 266 us, 6.0 TB/s; 288 with ordinary loads).
 template <class E, class W, int L, int Waves, int K, bool Ragged>
 __global__ void __launch_bounds__((Row<E, L, Waves, K, kBackThreads>::threads)) k_layer_norm_back(LnBackArgs g) {
     using R = Row<E, L, Waves, K, kBackThreads>;
@@ -489,8 +506,8 @@ __global__ void __launch_bounds__((Row<E, L, Waves, K, kBackThreads>::threads)) 
         const uint8_t* pdy = g.dy + row * g.lddy;
 #pragma unroll
         for (int k = 0; k < K; k++) {
-            d.x[k] = load_row<E, true>(px, a[k]);
-            d.dy[k] = load_row<E, true>(pdy, a[k]);
+            d.x[k] = load_row<E, !Ragged>(px, a[k]);
+            d.dy[k] = load_row<E, !Ragged>(pdy, a[k]);
         }
         d.mean = g.mean[row];
         d.rstd = g.rstd[row];
@@ -822,13 +839,14 @@ bool span_overlap(const void* p, uint64_t pn, const Rows& m, uint64_t rows, uint
 }
 
 // The layout of a row: lanes of a wave, or waves, and vectors per lane; calls
-// fn with the three as constants.  Short rows take 8 elements a lane; from 513
-// columns on a wave's own row takes 16, then 32 (16384 x 1600 bf16: 16.5 us,
-// 17.3 with two waves of 16; 16384 x 1024: 13.8 and 11.3).  The backward pass
-// holds two sums for each element, so its rows take 16 and spread over waves
-// sooner (32: 65536 x 1024 88 us against 74, 65536 x 4096 283 against 268); from
-// 8193 columns on 8 waves take 24, then 32 (8192 x 12288: 117 us; 124 with 16
-// waves of 16, whose blocks leave a lane 128 registers).
+// fn with the three as constants.  Each step keeps the lanes two thirds full or
+// better where that pays, since a row's fixed instructions count as much as its
+// elements' (12952 x 8309 bf16 forward: 86 us in 4 waves of 40, 161 in 8 of 32;
+// 16384 x 1600: 16.5 in a wave of 32, 17.3 in two of 16; 16384 x 1024: 11.3 in a
+// wave of 16, 13.8 in one of 32).  The backward pass holds two sums for each
+// element, so its rows take 16 and spread over waves sooner (32: 65536 x 1024 88
+// us against 74, 65536 x 4096 283 against 268); 24 between the powers of two, in
+// bf16 only (16384 x 2056: 46 us, 56 without; 16384 x 4099 fp32: 159 and 142).
 constexpr uint32_t kMaxCols = 32768, kMaxBackCols = 16384;       // beyond: the long forms
 
 template <int N>
@@ -836,24 +854,34 @@ using Int = std::integral_constant<int, N>;
 
 template <class E, bool Back, class Fn>
 auto with_row(uint32_t cols, Fn fn) {
-    constexpr int K8 = 8 / E::vec, K16 = 16 / E::vec, K32 = 32 / E::vec;
-    if (cols <= 64) return fn(Int<8>{}, Int<1>{}, Int<K8>{});
-    if (cols <= 128) return fn(Int<16>{}, Int<1>{}, Int<K8>{});
-    if (cols <= 256) return fn(Int<32>{}, Int<1>{}, Int<K8>{});
-    if (cols <= 512) return fn(Int<64>{}, Int<1>{}, Int<K8>{});
-    if (cols <= 1024) return fn(Int<64>{}, Int<1>{}, Int<K16>{});
+    const auto go = [&](auto l, auto waves, auto elements) { return fn(l, waves, Int<elements() / E::vec>{}); };
+    if (cols <= 64) return go(Int<8>{}, Int<1>{}, Int<8>{});
+    if (cols <= 128) return go(Int<16>{}, Int<1>{}, Int<8>{});
+    if (cols <= 256) return go(Int<16>{}, Int<1>{}, Int<16>{});
+    if (cols <= 512) return go(Int<32>{}, Int<1>{}, Int<16>{});
+    if (cols <= 1024) return go(Int<64>{}, Int<1>{}, Int<16>{});
     if constexpr (Back) {
-        if (cols <= 2048) return fn(Int<64>{}, Int<2>{}, Int<K16>{});
-        if (cols <= 4096) return fn(Int<64>{}, Int<4>{}, Int<K16>{});
-        if (cols <= 8192) return fn(Int<64>{}, Int<8>{}, Int<K16>{});
-        if (cols <= 12288) return fn(Int<64>{}, Int<8>{}, Int<24 / E::vec>{});
-        return fn(Int<64>{}, Int<8>{}, Int<K32>{});
+        constexpr bool bf16 = E::vec == 8;
+        if (bf16 && cols <= 1536) return go(Int<64>{}, Int<1>{}, Int<24>{});
+        if (cols <= 2048) return go(Int<64>{}, Int<2>{}, Int<16>{});
+        if (bf16 && cols <= 3072) return go(Int<64>{}, Int<2>{}, Int<24>{});
+        if (cols <= 4096) return go(Int<64>{}, Int<4>{}, Int<16>{});
+        if (bf16 && cols <= 6144) return go(Int<64>{}, Int<4>{}, Int<24>{});
+        if (cols <= 8192) return go(Int<64>{}, Int<8>{}, Int<16>{});
+        if (cols <= 12288) return go(Int<64>{}, Int<8>{}, Int<24>{});
+        return go(Int<64>{}, Int<8>{}, Int<32>{});
     } else {
-        if (cols <= 2048) return fn(Int<64>{}, Int<1>{}, Int<K32>{});
-        if (cols <= 4096) return fn(Int<64>{}, Int<2>{}, Int<K32>{});
-        if (cols <= 8192) return fn(Int<64>{}, Int<4>{}, Int<K32>{});
-        if (cols <= 16384) return fn(Int<64>{}, Int<8>{}, Int<K32>{});
-        return fn(Int<64>{}, Int<16>{}, Int<K32>{});
+        if (cols <= 1536) return go(Int<64>{}, Int<1>{}, Int<24>{});
+        if (cols <= 2048) return go(Int<64>{}, Int<1>{}, Int<32>{});
+        if (cols <= 3072) return go(Int<64>{}, Int<2>{}, Int<24>{});
+        if (cols <= 4096) return go(Int<64>{}, Int<2>{}, Int<32>{});
+        if (cols <= 6144) return go(Int<64>{}, Int<4>{}, Int<24>{});
+        if (cols <= 8192) return go(Int<64>{}, Int<4>{}, Int<32>{});
+        if (cols <= 10240) return go(Int<64>{}, Int<4>{}, Int<40>{});
+        if (cols <= 12288) return go(Int<64>{}, Int<4>{}, Int<48>{});
+        if (cols <= 16384) return go(Int<64>{}, Int<8>{}, Int<32>{});
+        if (cols <= 24576) return go(Int<64>{}, Int<8>{}, Int<48>{});
+        return go(Int<64>{}, Int<16>{}, Int<32>{});
     }
 }
 
@@ -972,7 +1000,12 @@ spccl_status_t launch_backward(const LnBackArgs& g, int32_t gdtype, void* dw, vo
         with_row<E, true>(g.cols, [&](auto l, auto waves, auto k) {
             using R = Row<E, l(), waves(), k(), kBackThreads>;
             const dim3 grid(back_blocks(g.rows, R::rows)), block(R::threads);
-            if (g.cols % E::vec) hipLaunchKernelGGL((k_layer_norm_back<E, W, l(), waves(), k(), true>), grid, block, 0, st, g);
+            // a misaligned row's vectors lie across lines, which streaming
+            // loads would fetch twice: it takes the ordinary ones (7434 x
+            // 5760 bf16, pitch 5761: 60 us, 81 streamed)
+            const bool odd = g.cols % E::vec || ((reinterpret_cast<uintptr_t>(g.x) | reinterpret_cast<uintptr_t>(g.dy) |
+                                                  g.ldx | g.lddy) & 15u);
+            if (odd) hipLaunchKernelGGL((k_layer_norm_back<E, W, l(), waves(), k(), true>), grid, block, 0, st, g);
             else hipLaunchKernelGGL((k_layer_norm_back<E, W, l(), waves(), k(), false>), grid, block, 0, st, g);
         });
     }
