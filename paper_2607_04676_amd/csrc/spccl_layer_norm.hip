@@ -680,14 +680,16 @@ __global__ void __launch_bounds__(1024) k_layer_norm_back_long(LnBackArgs g) {
     back_row<E, W, 1024>(g, blockIdx.x);
 }
 
-// A small backward pass in one launch: the first `column_blocks` blocks take
-// 256 columns each and add up all rows (8 waves every 8th row, then their
-// sums in order), the others write a row of dx each.  Every element is read
-// twice, from the caches.  In place, dx would be written over what a column
-// block has yet to read: then the two kinds of blocks are two launches
-// (first_block picks them), with the same bits.
+// A backward pass of few rows in one launch: the first blocks take 256 columns
+// and a strip of the rows each (8 waves every 8th row, then their sums in
+// order), the others write a row of dx each.  Every element is read twice, the
+// second time from the caches; in return a column has as many sums to join as
+// there are strips, not as there are CUs (a single strip's are final).  In
+// place, dx would be written over what a column block has yet to read: then the
+// two kinds of blocks are two launches (first_block picks them), with the same
+// bits.
 struct LnSmallArgs {
-    uint32_t column_blocks, first_block;
+    uint32_t columns, strips, first_block;    // column blocks: columns of them per strip
     void* dw;
     void* db;
     int accumulate;
@@ -696,18 +698,21 @@ constexpr uint32_t kSmallThreads = 512;
 template <class E, class W, class G>
 __global__ void __launch_bounds__(kSmallThreads) k_layer_norm_back_small(LnBackArgs g, LnSmallArgs o) {
     const uint32_t block = blockIdx.x + o.first_block;
-    if (block >= o.column_blocks) {
-        back_row<E, W, kSmallThreads>(g, block - o.column_blocks);
+    if (block >= o.columns * o.strips) {
+        back_row<E, W, kSmallThreads>(g, block - o.columns * o.strips);
         return;
     }
+    const uint32_t strip = block / o.columns, column = block % o.columns;
+    const uint32_t per = ((uint32_t)g.rows + o.strips - 1) / o.strips, first = strip * per;
+    const uint32_t end = first + per < (uint32_t)g.rows ? first + per : (uint32_t)g.rows;
     constexpr uint32_t waves = kSmallThreads / 64;
     __shared__ float s_sum[2][waves][256];
     const uint32_t wave = threadIdx.x >> 6, lane = threadIdx.x & 63u;
-    const uint32_t c = block * 256 + lane * 4;
+    const uint32_t c = column * 256 + lane * 4;
     const uint32_t rem = c < g.cols ? (g.cols - c < 4 ? g.cols - c : 4) : 0;
     float dw[4] = {0.f, 0.f, 0.f, 0.f}, db[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
-    for (uint32_t row = wave; row < (uint32_t)g.rows; row += waves) {
+    for (uint32_t row = first + wave; row < end; row += waves) {
         float x[4], dy[4];
         load_param<E, 4>(g.x + row * g.ldx, c, rem, 0.f, x);
         load_param<E, 4>(g.dy + row * g.lddy, c, rem, 0.f, dy);
@@ -726,11 +731,16 @@ __global__ void __launch_bounds__(kSmallThreads) k_layer_norm_back_small(LnBackA
     __syncthreads();
     const uint32_t which = threadIdx.x >> 8, col = threadIdx.x & 255u;
     typename G::raw* out = static_cast<typename G::raw*>(which ? o.db : o.dw);
-    const uint32_t at = block * 256 + col;
-    if (!out || at >= g.cols) return;
+    const uint32_t at = column * 256 + col;
+    if (at >= g.cols) return;
     float t = 0.f;
 #pragma unroll
     for (uint32_t q = 0; q < waves; q++) t += s_sum[which][q][col];
+    if (o.strips > 1) {
+        g.part[((uint64_t)strip * 2 + which) * g.cols + at] = t;
+        return;
+    }
+    if (!out) return;
     if (o.accumulate) t += G::one(out[at]);
     out[at] = G::round(t);
 }
@@ -938,31 +948,39 @@ spccl_status_t launch_forward(const LnArgs& g, hipStream_t st) {
 // none for less than two rounds of rows (307 x 11622: 25 us; one round 36, four
 // 29).
 constexpr uint32_t kStrips = 64;
+static_assert(kStrips <= kBackBlocks, "k_layer_norm_grads adds up to kBackBlocks parts");
 uint32_t back_blocks(uint64_t rows, uint32_t rows_per_block) {
     const uint64_t b = (rows + 2 * rows_per_block - 1) / (2 * rows_per_block);
     return (uint32_t)(b < kBackBlocks ? b : kBackBlocks);
 }
 uint32_t strips(uint64_t rows) { return (uint32_t)(rows < kStrips ? rows : kStrips); }
 
+// Backward passes of up to 1024 rows in bf16, 512 in fp32, are taken by
+// k_layer_norm_back_small at any width: reading their rows twice moves less
+// than a pair of sums per column and CU (us with the host's part, so / by
+// k_layer_norm_back, bf16: 64 x 1024 9.7 / 12.9, 256 x 8192 12.3 / 17.1, 512 x
+// 16384 22 / 40, 1024 x 8192 19 / 26, 1536 x 16384 60 / 55; fp32: 512 x 4096
+// 12.1 / 13.2, 1024 x 4096 18.6 / 16.5).  Strips of 64 rows beyond 128.
+template <class E>
+bool small_backward(uint64_t rows) {
+    return rows * sizeof(typename E::raw) <= 2048;
+}
+inline uint32_t small_strips(uint64_t rows) { return rows <= 128 ? 1 : (uint32_t)((rows + 63) / 64); }
+
 template <class E>
 uint32_t back_parts(uint64_t rows, uint32_t cols) {
+    if (small_backward<E>(rows)) return small_strips(rows);
     if (cols > kMaxBackCols || cols < (uint32_t)E::vec) return strips(rows);
     return with_row<E, true>(cols, [&](auto l, auto waves, auto k) {
         return back_blocks(rows, Row<E, l(), waves(), k(), kBackThreads>::rows);
     });
 }
 
-// Backward passes of so few rows take one launch, k_layer_norm_back_small, at
-// any width (us with the host's part, small / otherwise, bf16: 64 x 1024 9.7 /
-// 12.9, 128 x 8192 9.6 / 16.1, 128 x 131072 46 / 105; with 256 rows 13.3 / 12.8
-// at 1024 columns and 24 / 20 at 8192).
-constexpr uint64_t kSmallRows = 128;
-
 template <class E, class W>
 spccl_status_t launch_small(const LnBackArgs& g, int32_t gdtype, void* dw, void* db, int32_t accumulate, bool in_place,
                             hipStream_t st) {
-    LnSmallArgs o{g.part ? (g.cols + 255) / 256 : 0, 0, dw, db, accumulate};
-    const uint32_t rows = g.dx ? (uint32_t)g.rows : 0;
+    LnSmallArgs o{(g.cols + 255) / 256, g.part ? small_strips(g.rows) : 0, 0, dw, db, accumulate};
+    const uint32_t rows = g.dx ? (uint32_t)g.rows : 0, sums = o.columns * o.strips;
     const auto go = [&](uint32_t first, uint32_t count) {
         if (!count) return SPCCL_OK;
         o.first_block = first;
@@ -972,16 +990,32 @@ spccl_status_t launch_small(const LnBackArgs& g, int32_t gdtype, void* dw, void*
             hipLaunchKernelGGL((k_layer_norm_back_small<E, W, F32>), dim3(count), dim3(kSmallThreads), 0, st, g, o);
         return launch_status();
     };
-    if (!in_place) return go(0, o.column_blocks + rows);
-    const spccl_status_t st1 = go(0, o.column_blocks);
-    return st1 == SPCCL_OK ? go(o.column_blocks, rows) : st1;
+    if (!in_place) return go(0, sums + rows);
+    const spccl_status_t st1 = go(0, sums);
+    return st1 == SPCCL_OK ? go(sums, rows) : st1;
+}
+
+spccl_status_t launch_grads(const float* part, uint32_t parts, uint32_t cols, int32_t gdtype, void* dw, void* db,
+                            int32_t accumulate, hipStream_t st) {
+    const dim3 grid((uint32_t)((2ull * cols + 63) / 64)), block(1024);
+    if (gdtype == kBF16)
+        hipLaunchKernelGGL(k_layer_norm_grads<BF16>, grid, block, 0, st, part, parts, cols, static_cast<uint16_t*>(dw),
+                           static_cast<uint16_t*>(db), accumulate);
+    else
+        hipLaunchKernelGGL(k_layer_norm_grads<F32>, grid, block, 0, st, part, parts, cols, static_cast<uint32_t*>(dw),
+                           static_cast<uint32_t*>(db), accumulate);
+    return launch_status();
 }
 
 template <class E, class W>
 spccl_status_t launch_backward(const LnBackArgs& g, int32_t gdtype, void* dw, void* db, int32_t accumulate,
                                hipStream_t st) {
-    if (g.rows <= kSmallRows)
-        return launch_small<E, W>(g, gdtype, dw, db, accumulate, g.dx && (g.dx == g.x || g.dx == g.dy), st);
+    if (small_backward<E>(g.rows)) {
+        const bool in_place = g.dx && (g.dx == g.x || g.dx == g.dy);
+        const spccl_status_t st1 = launch_small<E, W>(g, gdtype, dw, db, accumulate, in_place, st);
+        if (st1 != SPCCL_OK || !g.part || small_strips(g.rows) == 1) return st1;
+        return launch_grads(g.part, small_strips(g.rows), g.cols, gdtype, dw, db, accumulate, st);
+    }
     if (g.cols > kMaxBackCols || g.cols < (uint32_t)E::vec) {
         // the columns' sums first: dx may be written over dy or x
         if (g.part) {
@@ -1011,15 +1045,7 @@ spccl_status_t launch_backward(const LnBackArgs& g, int32_t gdtype, void* dw, vo
     }
     if (launch_status() != SPCCL_OK) return SPCCL_ERR_HIP;
     if (!g.part) return SPCCL_OK;
-    const uint32_t parts = back_parts<E>(g.rows, g.cols);
-    const dim3 grid((uint32_t)((2ull * g.cols + 63) / 64)), block(1024);
-    if (gdtype == kBF16)
-        hipLaunchKernelGGL(k_layer_norm_grads<BF16>, grid, block, 0, st, g.part, parts, g.cols,
-                           static_cast<uint16_t*>(dw), static_cast<uint16_t*>(db), accumulate);
-    else
-        hipLaunchKernelGGL(k_layer_norm_grads<F32>, grid, block, 0, st, g.part, parts, g.cols,
-                           static_cast<uint32_t*>(dw), static_cast<uint32_t*>(db), accumulate);
-    return launch_status();
+    return launch_grads(g.part, back_parts<E>(g.rows, g.cols), g.cols, gdtype, dw, db, accumulate, st);
 }
 
 }  // namespace

@@ -204,6 +204,33 @@ def test_backward(S, rows, cols, dtype, wdtype, gdtype, accumulate):
     assert bool((whole[scratch.numel():] == 0xFF).all())
 
 
+@pytest.mark.parametrize("rows,cols", [(128, 300), (129, 300), (192, 257), (193, 4100), (512, 100), (513, 100), (1024, 1030),
+                                       (1025, 1030), (130, 20_001)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_backward_around_the_strips_of_rows(S, rows, cols, dtype):
+    """Row counts where a few rows' launch takes another strip or ends, also in place."""
+    log(f"layer norm backward strips {rows}x{cols} {dtype}")
+    x, dy = matrix(rows, cols, dtype, 1, 2.0, 0.5), matrix(rows, cols, dtype, 2)
+    w = vector(cols, "f32", 3, 0.3, 1.0)
+    mean = x.float().mean(1)
+    rstd = 1.0 / (x.float().var(1, unbiased=False) + 1e-5).sqrt()
+    (ex, bx), (ew, bw), (eb, bb) = backward_bounds(dy, x, w, mean, rstd, dtype)
+    first = None
+    for over in ("apart", "x", "dy"):
+        a, b = dy.clone(), x.clone()
+        dx = {"apart": torch.empty_like(x), "x": b, "dy": a}[over]
+        dw, db = torch.empty(cols, device="cuda"), torch.empty(cols, device="cuda")
+        scratch, whole = scratch_for(S, rows, cols)
+        S.spccl_layer_norm_backward(a, b, w, mean, rstd, dx, dw, db, scratch)
+        torch.cuda.synchronize()
+        within(dx, ex, bx, "dx")
+        within(dw, ew, bw + OUT["f32"] * ew.abs(), "dweight")
+        within(db, eb, bb + OUT["f32"] * eb.abs(), "dbias")
+        assert bool((whole[scratch.numel():] == 0xFF).all())
+        first = first or (dx.clone(), dw, db)
+        assert all(torch.equal(p, q) for p, q in zip(first, (dx, dw, db)))
+
+
 @pytest.mark.parametrize("rows,cols", [(70, 1600), (40, 128), (12, 5000), (9, 20_000)])
 def test_backward_of_parts_in_place_and_twice(S, rows, cols):
     """Each gradient alone, dx over dy or over x, and equal bits from equal calls."""
