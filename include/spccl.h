@@ -2,7 +2,8 @@
  * spccl.h -- C ABI of the MI355X (gfx950) Pici hot path of SpCCL
  * (arXiv 2607.04676): dense <-> Pici codec, elementwise reduction with
  * fill-in, gather-expand, and ring collectives over P virtual ranks held in
- * one GPU's memory.
+ * one GPU's memory; and the steps of a training loop around them: layer norm,
+ * pruning with error feedback, AdamW.
  *
  * Conventions for every entry point:
  *  - Pointers are device pointers unless marked "host".  Messages and
@@ -529,7 +530,9 @@ spccl_status_t spccl_prune(const void* grad, float* residual, const float* thres
  * may be short).  A scale brings its block's largest magnitude into [2^7,
  * 2^8).  8-bit moments are rounded stochastically; a second moment above zero
  * stays at least the smallest value; a block that holds a NaN or an infinity
- * has the scale 255 and stands for NaN.  All-zero bytes are zero moments. */
+ * has the scale 255 and stands for NaN.  Scales are otherwise written as 25 to
+ * 247; a scale of 0 stands for a block of zeros, so all-zero bytes are zero
+ * moments. */
 typedef enum { SPCCL_STATE_F32 = 0, SPCCL_STATE_F8 = 1 } spccl_state_t;
 #define SPCCL_STATE_BLOCK 32
 
@@ -566,9 +569,10 @@ typedef struct {
 
 /* Lays a plan for `count` tensors (host array) out in `table` (device, 16-byte
  * aligned, spccl_adamw_plan_bytes(tensors, count) bytes, which the plan uses
- * until it is dropped), with small kernels on `stream`.  Refuses overlaps of
- * anything a step writes with anything else (SPCCL_ERR_INVALID_ARG); gradients
- * may be shared.  COO gradients: SPCCL_ERR_UNSUPPORTED. */
+ * until it is dropped), with small kernels on `stream`: a step on another
+ * stream has to wait for them.  Refuses overlaps of anything a step writes
+ * with anything else (SPCCL_ERR_INVALID_ARG); gradients may be shared.  COO
+ * gradients: SPCCL_ERR_UNSUPPORTED. */
 uint64_t spccl_adamw_plan_bytes(const spccl_adamw_tensor_t* tensors, int32_t count);
 spccl_status_t spccl_adamw_plan(const spccl_adamw_tensor_t* tensors, int32_t count, int32_t param_dtype, int32_t grad_dtype,
                                 int32_t state, void* table, uint64_t table_bytes, spccl_adamw_plan_t* plan, void* stream);
