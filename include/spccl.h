@@ -490,7 +490,8 @@ spccl_status_t spccl_layer_norm(const void* x, uint64_t ldx, const void* weight,
  *   dx = rstd * (g - avg(g) - h * avg(g * h))    (averages over the row),
  *   dweight = sum over the rows of dy * h,  dbias = sum over the rows of dy.
  * mean and rstd are the forward pass's.  dx (NULL: not wanted) has `dtype` and
- * may be dy or x itself (same pitch).  dweight and dbias (either NULL: not
+ * may be dy or x itself (same pitch); no other overlap of an output or of the
+ * scratch.  dweight and dbias (either NULL: not
  * wanted) have `gdtype`; with accumulate != 0 the sums are added to what is
  * there, as a gradient bucket collects micro-batches, otherwise they replace
  * it (zeros if rows == 0).  Sums over the rows are held in fp32 and their

@@ -847,6 +847,24 @@ bool span_overlap(const void* p, uint64_t pn, const Rows& m, uint64_t rows, uint
     const uintptr_t x = reinterpret_cast<uintptr_t>(p), y = reinterpret_cast<uintptr_t>(m.p);
     return x < y + ((rows - 1) * m.ld + cols) * s && y < x + pn;
 }
+// Whether an array that is written shares a byte with another of the call.
+struct Span {
+    const void* p;
+    uint64_t bytes;
+};
+template <size_t Written, size_t Read>
+bool spans_overlap(const Span (&w)[Written], const Span (&r)[Read]) {
+    const auto meet = [](const Span& a, const Span& b) {
+        return a.p && b.p && span_overlap(a.p, a.bytes, Rows{b.p, b.bytes}, 1, b.bytes, 1);
+    };
+    for (size_t i = 0; i < Written; i++) {
+        for (size_t j = 0; j < i; j++)
+            if (meet(w[i], w[j])) return true;
+        for (const Span& b : r)
+            if (meet(w[i], b)) return true;
+    }
+    return false;
+}
 
 // The layout of a row: lanes of a wave, or waves, and vectors per lane; calls
 // fn with the three as constants.  Each step keeps the lanes two thirds full or
@@ -1073,6 +1091,8 @@ spccl_status_t spccl_layer_norm(const void* x, uint64_t ldx, const void* weight,
             return SPCCL_ERR_INVALID_ARG;
     if (span_overlap(weight, ws * cols, ry, rows, cols, s) || span_overlap(bias, ws * cols, ry, rows, cols, s))
         return SPCCL_ERR_INVALID_ARG;
+    const Span statistics[2] = {{mean, 4 * rows}, {rstd, 4 * rows}}, params[2] = {{weight, ws * cols}, {bias, ws * cols}};
+    if (spans_overlap(statistics, params)) return SPCCL_ERR_INVALID_ARG;
     const LnArgs g{static_cast<const uint8_t*>(x), static_cast<const uint8_t*>(weight), static_cast<const uint8_t*>(bias),
                    static_cast<uint8_t*>(y), mean, rstd, ldx * s, ldy * s, rows, (uint32_t)cols, (float)eps};
     const hipStream_t st = reinterpret_cast<hipStream_t>(stream);
@@ -1118,10 +1138,9 @@ spccl_status_t spccl_layer_norm_backward(const void* dy, uint64_t lddy, const vo
         if (span_overlap(dweight, gs * cols, m, rows, cols, s) || span_overlap(dbias, gs * cols, m, rows, cols, s) ||
             (need && span_overlap(scratch, need, m, rows, cols, s)))
             return SPCCL_ERR_INVALID_ARG;
-    const Rows one[2] = {{dweight, cols}, {dbias, cols}};
-    if (span_overlap(dweight, gs * cols, one[1], 1, cols, gs)) return SPCCL_ERR_INVALID_ARG;
-    for (const Rows& m : one)
-        if (need && span_overlap(scratch, need, m, 1, cols, gs)) return SPCCL_ERR_INVALID_ARG;
+    const Span sums[3] = {{dweight, gs * cols}, {dbias, gs * cols}, {need ? scratch : nullptr, need}};
+    const Span read[3] = {{weight, elem_bytes(wdtype) * cols}, {mean, 4 * rows}, {rstd, 4 * rows}};
+    if (spans_overlap(sums, read)) return SPCCL_ERR_INVALID_ARG;
     const LnBackArgs g{static_cast<const uint8_t*>(dy), static_cast<const uint8_t*>(x), static_cast<const uint8_t*>(weight),
                        mean, rstd, static_cast<uint8_t*>(dx), grads ? static_cast<float*>(scratch) : nullptr,
                        lddy * s, ldx * s, lddx * s, rows, (uint32_t)cols};

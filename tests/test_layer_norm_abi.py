@@ -72,3 +72,21 @@ def test_scratch_bytes(S):
     assert f(1, 1) >= 8
     for cols in (1, 100, 1600, 20_000, 100_000):             # a bounded number of sums per column
         assert f((1 << 31) - 1, cols) <= 8 * cols * 4096
+
+
+def test_overlaps_of_vectors(S):
+    # statistics are written while other rows still read the weight and the bias
+    for out in ("mean", "rstd"):
+        for read in (40 * MB, 41 * MB):
+            assert forward(S, **{out: read}) == INVALID
+            assert forward(S, **{out: read + 396}) == INVALID
+            assert forward(S, **{out: read - 36}) == INVALID
+    assert forward(S, mean=50 * MB, rstd=50 * MB + 36) == INVALID
+    # and the sums of the columns while others read the weight and the statistics
+    for out in ("dw", "db", "scratch"):
+        for read, size in ((40 * MB, 400), (50 * MB, 40), (51 * MB, 40)):
+            assert backward(S, **{out: read}) == INVALID
+            if out != "scratch":
+                assert backward(S, **{out: read + size - 4}) == INVALID
+                assert backward(S, **{out: read - 396}) == INVALID
+    assert backward(S, scratch=61 * MB) == INVALID
