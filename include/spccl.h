@@ -475,7 +475,7 @@ spccl_status_t spccl_vr_all_reduce_sliced(void* const* send, void* const* recv, 
 /* ---- layer norm (a layer of the models whose gradients the collectives reduce) -- */
 
 /* y = (x - mean) * rstd * weight + bias over each row of a matrix of `rows`
- * rows and `cols` columns (rows < 2^31, 1 <= cols < 2^27), mean and
+ * rows and `cols` columns (rows < 2^31, 1 <= cols < 2^26), mean and
  * 1 / sqrt(variance + eps) taken over the row (the biased variance).  ldx, ldy: elements between
  * rows (>= cols).  x and y have `dtype`, weight and bias (NULL: ones, zeros)
  * `wdtype`; sums are held in fp32 and y is rounded once.  mean and rstd

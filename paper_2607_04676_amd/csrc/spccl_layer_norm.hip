@@ -875,6 +875,10 @@ bool spans_overlap(const Span (&w)[Written], const Span (&r)[Read]) {
 // element, so its rows take 16 and spread over waves sooner (32: 65536 x 1024 88
 // us against 74, 65536 x 4096 283 against 268); 24 between the powers of two, in
 // bf16 only (16384 x 2056: 46 us, 56 without; 16384 x 4099 fp32: 159 and 142).
+// Columns of any call stay below 2^26: k_layer_norm_grads takes 1024 threads for
+// 32 of them, k_layer_norm_back_small up to 16 strips of 512 for 256, and a grid
+// has fewer than 2^32 threads.
+constexpr uint64_t kColsLimit = 1ull << 26;
 constexpr uint32_t kMaxCols = 32768, kMaxBackCols = 16384;       // beyond: the long forms
 
 template <int N>
@@ -1077,7 +1081,7 @@ spccl_status_t spccl_layer_norm(const void* x, uint64_t ldx, const void* weight,
                                 float* mean, float* rstd, uint64_t rows, uint64_t cols, int32_t dtype, int32_t wdtype,
                                 double eps, void* stream) {
     if (!dtype_ok(dtype) || !dtype_ok(wdtype)) return SPCCL_ERR_UNSUPPORTED;
-    if (rows >= (1ull << 31) || cols >= (1ull << 27)) return SPCCL_ERR_UNSUPPORTED;
+    if (rows >= (1ull << 31) || cols >= kColsLimit) return SPCCL_ERR_UNSUPPORTED;
     if (cols == 0 || ldx < cols || ldy < cols || !(eps >= 0.0)) return SPCCL_ERR_INVALID_ARG;
     if (rows == 0) return SPCCL_OK;
     if (!x || !y || !aligned(x, dtype) || !aligned(y, dtype) || !aligned(weight, wdtype) || !aligned(bias, wdtype) ||
@@ -1101,7 +1105,7 @@ spccl_status_t spccl_layer_norm(const void* x, uint64_t ldx, const void* weight,
 }
 
 uint64_t spccl_layer_norm_scratch_bytes(uint64_t rows, uint64_t cols) {
-    if (rows == 0 || rows >= (1ull << 31) || cols == 0 || cols >= (1ull << 27)) return 0;
+    if (rows == 0 || rows >= (1ull << 31) || cols == 0 || cols >= kColsLimit) return 0;
     const uint32_t a = back_parts<F32>(rows, (uint32_t)cols), b = back_parts<BF16>(rows, (uint32_t)cols);
     return 8ull * cols * (a > b ? a : b);
 }
@@ -1112,7 +1116,7 @@ spccl_status_t spccl_layer_norm_backward(const void* dy, uint64_t lddy, const vo
                                          int32_t gdtype, int32_t accumulate, void* scratch, uint64_t scratch_bytes,
                                          void* stream) {
     if (!dtype_ok(dtype) || !dtype_ok(wdtype) || !dtype_ok(gdtype)) return SPCCL_ERR_UNSUPPORTED;
-    if (rows >= (1ull << 31) || cols >= (1ull << 27)) return SPCCL_ERR_UNSUPPORTED;
+    if (rows >= (1ull << 31) || cols >= kColsLimit) return SPCCL_ERR_UNSUPPORTED;
     if (cols == 0 || lddy < cols || ldx < cols || (dx && lddx < cols)) return SPCCL_ERR_INVALID_ARG;
     if (!aligned(dweight, gdtype) || !aligned(dbias, gdtype)) return SPCCL_ERR_INVALID_ARG;
     const bool grads = dweight || dbias;

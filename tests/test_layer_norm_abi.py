@@ -90,3 +90,16 @@ def test_overlaps_of_vectors(S):
                 assert backward(S, **{out: read + size - 4}) == INVALID
                 assert backward(S, **{out: read - 396}) == INVALID
     assert backward(S, scratch=61 * MB) == INVALID
+
+
+def test_columns_that_a_grid_cannot_take(S):
+    # the reduction of the weight's gradient takes 1024 threads for 32 columns, of fewer than 2^32
+    for cols in (1 << 26, (1 << 27) - 1):
+        wide = dict(cols=cols, rows=0)
+        assert forward(S, ldx=cols, ldy=cols, **wide) == UNSUPPORTED
+        assert backward(S, ldx=cols, lddy=cols, lddx=cols, **wide) == UNSUPPORTED
+        assert S.spccl_layer_norm_scratch_bytes(10, cols) == 0
+    cols = (1 << 26) - 1
+    assert forward(S, cols=cols, rows=0, ldx=cols, ldy=cols) == OK
+    assert backward(S, cols=cols, rows=0, ldx=cols, lddy=cols, lddx=cols, dw=None, db=None) == OK
+    assert S.spccl_layer_norm_scratch_bytes(10, cols) == 8 * cols
