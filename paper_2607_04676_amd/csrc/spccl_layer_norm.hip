@@ -495,37 +495,49 @@ __global__ void __launch_bounds__((Row<E, L, Waves, K, kBackThreads>::threads)) 
     Params<E, W, K> w;
     w.load(g.w, a, 1.f);
     const float inv = 1.0f / (float)g.cols;
-    // a row's data; a group past the last row takes the last one along
+    // a row's data; a group past the last row reads the start of its block's
+    // first row instead, a line a load (600 x 12000 fp32: 30.7 us; 33.2 where
+    // every block's groups read the whole last row, 8192 x 12288 220 and 222)
     struct Data {
         u32x4 x[K], dy[K];
         float mean, rstd;
     };
-    const auto fetch = [&](uint64_t r0, Data& d) {
-        const uint64_t row = r0 + group < g.rows ? r0 + group : g.rows - 1;
-        const uint8_t* px = g.x + row * g.ldx;
-        const uint8_t* pdy = g.dy + row * g.lddy;
+    struct Source {
+        uint64_t row;
+        uint32_t mask;
+    };
+    const uint64_t first = (uint64_t)blockIdx.x * R::rows;
+    const auto source = [&](uint64_t r0) {
+        const bool mine = r0 + group < g.rows;
+        return Source{mine ? r0 + group : first, mine ? ~0u : 0u};
+    };
+    const auto fetch = [&](const Source& s, Data& d) {
+        const uint8_t* px = g.x + s.row * g.ldx;
+        const uint8_t* pdy = g.dy + s.row * g.lddy;
 #pragma unroll
         for (int k = 0; k < K; k++) {
-            d.x[k] = load_row<E, !Ragged>(px, a[k]);
-            d.dy[k] = load_row<E, !Ragged>(pdy, a[k]);
+            d.x[k] = load_row<E, !Ragged>(px, a[k] & s.mask);
+            d.dy[k] = load_row<E, !Ragged>(pdy, a[k] & s.mask);
         }
-        d.mean = g.mean[row];
-        d.rstd = g.rstd[row];
+        d.mean = g.mean[s.row];
+        d.rstd = g.rstd[s.row];
     };
     // the next row is on its way while this one is worked on, where the
-    // registers for it are there (not for 32 fp32 elements a lane)
+    // registers for it are there (not for 32 fp32 elements a lane; there, loading
+    // each of its vectors as soon as this row's is stored took 8192 x 16384 from
+    // 310 us to 302, but 3001 x 12289 from 98 to 101 and 600 x 16384 from 42 to 43)
     constexpr bool Ahead = K <= 6;
     const uint64_t step = (uint64_t)gridDim.x * R::rows;
     uint32_t turn = 0;
     Data next;
-    if constexpr (Ahead) fetch((uint64_t)blockIdx.x * R::rows, next);
-    for (uint64_t r0 = (uint64_t)blockIdx.x * R::rows; r0 < g.rows; r0 += step, turn ^= 1) {
+    if constexpr (Ahead) fetch(source(first), next);
+    for (uint64_t r0 = first; r0 < g.rows; r0 += step, turn ^= 1) {
         Data now;
         if constexpr (Ahead) {
             now = next;
-            fetch(r0 + step, next);
+            fetch(source(r0 + step), next);
         } else {
-            fetch(r0, now);
+            fetch(source(r0), now);
         }
         const bool mine = R::rows == 1 || r0 + group < g.rows;
         const uint64_t row = r0 + group;
@@ -537,7 +549,7 @@ __global__ void __launch_bounds__((Row<E, L, Waves, K, kBackThreads>::threads)) 
         for (int k = 0; k < K; k++) {
             w.pin(k);
             At((k * R::lanes + i) * V, mine ? g.cols : 0).clear(dy[k]);
-            // in place, the last row may already be written over (0 times a NaN is one)
+            // in place, the block's first row is already written over (0 times a NaN is one)
             if (R::rows > 1) x[k] = mine ? x[k] : u32x4{0, 0, 0, 0};
 #pragma unroll
             for (int j = 0; j < V; j++) {
@@ -866,6 +878,11 @@ bool spans_overlap(const Span (&w)[Written], const Span (&r)[Read]) {
     return false;
 }
 
+// Columns of any call stay below 2^26: k_layer_norm_grads takes 1024 threads for
+// 32 of them, k_layer_norm_back_small up to 16 strips of 512 for 256, and a grid
+// has fewer than 2^32 threads.
+constexpr uint64_t kColsLimit = 1ull << 26;
+
 // The layout of a row: lanes of a wave, or waves, and vectors per lane; calls
 // fn with the three as constants.  Each step keeps the lanes two thirds full or
 // better where that pays, since a row's fixed instructions count as much as its
@@ -875,10 +892,6 @@ bool spans_overlap(const Span (&w)[Written], const Span (&r)[Read]) {
 // element, so its rows take 16 and spread over waves sooner (32: 65536 x 1024 88
 // us against 74, 65536 x 4096 283 against 268); 24 between the powers of two, in
 // bf16 only (16384 x 2056: 46 us, 56 without; 16384 x 4099 fp32: 159 and 142).
-// Columns of any call stay below 2^26: k_layer_norm_grads takes 1024 threads for
-// 32 of them, k_layer_norm_back_small up to 16 strips of 512 for 256, and a grid
-// has fewer than 2^32 threads.
-constexpr uint64_t kColsLimit = 1ull << 26;
 constexpr uint32_t kMaxCols = 32768, kMaxBackCols = 16384;       // beyond: the long forms
 
 template <int N>
