@@ -573,7 +573,8 @@ typedef struct {
  * until it is dropped), with small kernels on `stream`: a step on another
  * stream has to wait for them.  Refuses overlaps of anything a step writes
  * with anything else (SPCCL_ERR_INVALID_ARG); gradients may be shared.  COO
- * gradients: SPCCL_ERR_UNSUPPORTED. */
+ * gradients: SPCCL_ERR_UNSUPPORTED.  A table that the HIP runtime does not know
+ * as memory a kernel can reach: SPCCL_ERR_HIP, before the first launch. */
 uint64_t spccl_adamw_plan_bytes(const spccl_adamw_tensor_t* tensors, int32_t count);
 spccl_status_t spccl_adamw_plan(const spccl_adamw_tensor_t* tensors, int32_t count, int32_t param_dtype, int32_t grad_dtype,
                                 int32_t state, void* table, uint64_t table_bytes, spccl_adamw_plan_t* plan, void* stream);

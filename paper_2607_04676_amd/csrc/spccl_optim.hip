@@ -636,6 +636,21 @@ spccl_status_t check_spans(const spccl_adamw_tensor_t* t, int32_t count, int32_t
     return st;
 }
 
+// Whether the runtime knows both ends of a range as memory that a kernel can
+// reach (also true inside an allocation).  The failed query is taken out of the
+// runtime's last error.
+bool reachable(const void* p, uint64_t bytes) {
+    for (const uint64_t at : {uint64_t{0}, bytes - 1}) {
+        hipPointerAttribute_t a{};
+        if (hipPointerGetAttributes(&a, static_cast<const uint8_t*>(p) + at) != hipSuccess) {
+            (void)hipGetLastError();
+            return false;
+        }
+        if (a.type == hipMemoryTypeUnregistered) return false;
+    }
+    return true;
+}
+
 template <int PT, int GT, bool Eight>
 spccl_status_t launch_adamw(const spccl_adamw_plan_t& plan, AdamArgs a, hipStream_t st) {
     constexpr uint64_t most = 0xFFFFFFFFu / kThreads;            // a grid has fewer than 2^32 threads
@@ -700,6 +715,9 @@ spccl_status_t spccl_adamw_plan(const spccl_adamw_tensor_t* tensors, int32_t cou
     if (bytes < need) return SPCCL_ERR_WORKSPACE;
     spccl_status_t st = check_spans(tensors, count, param_dtype, state, table, need);
     if (st != SPCCL_OK) return st;
+    // the kernels below write the table at once: an address that is none of the
+    // device's would fault there
+    if (need && !reachable(table, need)) return SPCCL_ERR_HIP;
     AdamTensor* entries = static_cast<AdamTensor*>(table);
     uint32_t* chunk = reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(table) + (uint64_t)count * sizeof(AdamTensor));
     uint64_t next[2] = {0, arrays}, counter = 0;

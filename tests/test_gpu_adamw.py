@@ -9,6 +9,8 @@ adds 2 u more); an update m / (sqrt(v) c + eps) * rate is within 12 u of itself
 beyond what its moments bring (sqrt halves v's), and param (1 - lr wd) within
 3 u.
 """
+import ctypes
+
 import numpy as np
 import pytest
 
@@ -566,3 +568,42 @@ def test_binding_refuses(S):
     plan = S.spccl_adamw_plan([S.adamw_tensor(new(), new(), new(), new())], table)
     with pytest.raises(ValueError):
         S.spccl_adamw_step(plan, table[:256], 1e-3, grad_scale=torch.zeros(2, device="cuda"))
+
+
+def test_a_table_that_is_no_device_memory_is_refused(S):
+    """Addresses that the device cannot reach are an error of the call, before
+    its first launch: one that nothing lies at, and host memory."""
+    log("adamw table elsewhere")
+    new = lambda: torch.zeros(1000, device="cuda")  # noqa: E731
+    tensors = [S.adamw_tensor(new(), new(), new(), new())]
+    arr = (S.spccl_adamw_tensor_t * 1)(*tensors)
+    need = S.spccl_adamw_plan_bytes(tensors)
+    host = torch.zeros(need + 16, dtype=torch.uint8)
+    p = S.spccl_adamw_plan_t()
+    call = lambda table: S._lib.spccl_adamw_plan(arr, 1, S.SPCCL_F32, S.SPCCL_F32, S.SPCCL_STATE_F32, table, need,  # noqa: E731
+                                                 ctypes.byref(p), None)
+    for table in (100 << 20, -(-host.data_ptr() // 16) * 16):
+        assert call(table) == 6
+        assert p.magic == 0
+    # the refusal leaves no error behind, and a real table is taken
+    torch.cuda.synchronize()
+    table = torch.empty(need, dtype=torch.uint8, device="cuda")
+    assert call(table.data_ptr()) == 0
+    torch.cuda.synchronize()
+
+
+def test_a_shared_gradient(S):
+    """Two tensors may read one gradient: each takes the step it takes alone."""
+    log("adamw shared gradient")
+    g = torch.full((1000,), 0.25, device="cuda")
+    sets = [[torch.full((1000,), float(k), device="cuda"), *(torch.zeros(1000, device="cuda") for _ in range(2))]
+            for k in (1, 2, 1, 2)]
+    ws = torch.zeros(256, dtype=torch.uint8, device="cuda")
+    for group in (sets[:2], sets[2:3], sets[3:]):
+        tensors = [S.adamw_tensor(p, g, m, v) for p, m, v in group]
+        table = torch.empty(S.spccl_adamw_plan_bytes(tensors), dtype=torch.uint8, device="cuda")
+        S.spccl_adamw_step(S.spccl_adamw_plan(tensors, table), ws, 1e-3)
+    torch.cuda.synchronize()
+    for a, b in zip(sets[0] + sets[1], sets[2] + sets[3]):
+        assert torch.equal(a, b)
+    assert float(sets[0][0][0]) < 1.0
