@@ -468,6 +468,7 @@ struct LnBackArgs {
 };
 
 constexpr uint32_t kBackThreads = 512;
+__device__ const float kNoRow = 0.f;          // the mean and rstd of a group without a row
 
 // Each group of lanes walks over rows, keeping its columns' sums of dy h and
 // dy in registers; a block joins its groups' through LDS, in their order, and
@@ -502,14 +503,20 @@ __global__ void __launch_bounds__((Row<E, L, Waves, K, kBackThreads>::threads)) 
         u32x4 x[K], dy[K];
         float mean, rstd;
     };
+    // (its mean and rstd are zeros: the deviation of a zero from another row's mean
+    // may be infinite, and 0 times that is NaN)
     struct Source {
         uint64_t row;
         uint32_t mask;
+        const float* mean;
+        const float* rstd;
     };
     const uint64_t first = (uint64_t)blockIdx.x * R::rows;
     const auto source = [&](uint64_t r0) {
         const bool mine = r0 + group < g.rows;
-        return Source{mine ? r0 + group : first, mine ? ~0u : 0u};
+        const uint64_t row = mine ? r0 + group : first;
+        const bool stats = mine || R::rows == 1;                     // a lone group ends with its last row
+        return Source{row, mine ? ~0u : 0u, stats ? g.mean + row : &kNoRow, stats ? g.rstd + row : &kNoRow};
     };
     const auto fetch = [&](const Source& s, Data& d) {
         const uint8_t* px = g.x + s.row * g.ldx;
@@ -519,8 +526,8 @@ __global__ void __launch_bounds__((Row<E, L, Waves, K, kBackThreads>::threads)) 
             d.x[k] = load_row<E, !Ragged>(px, a[k] & s.mask);
             d.dy[k] = load_row<E, !Ragged>(pdy, a[k] & s.mask);
         }
-        d.mean = g.mean[s.row];
-        d.rstd = g.rstd[s.row];
+        d.mean = *s.mean;
+        d.rstd = *s.rstd;
     };
     // the next row is on its way while this one is worked on, where the
     // registers for it are there (not for 32 fp32 elements a lane; there, loading
@@ -549,7 +556,7 @@ __global__ void __launch_bounds__((Row<E, L, Waves, K, kBackThreads>::threads)) 
         for (int k = 0; k < K; k++) {
             w.pin(k);
             At((k * R::lanes + i) * V, mine ? g.cols : 0).clear(dy[k]);
-            // in place, the block's first row is already written over (0 times a NaN is one)
+            // (in place, the block's first row is already written over)
             if (R::rows > 1) x[k] = mine ? x[k] : u32x4{0, 0, 0, 0};
 #pragma unroll
             for (int j = 0; j < V; j++) {
@@ -651,10 +658,18 @@ __device__ __forceinline__ void back_row(const LnBackArgs& g, uint64_t row) {
         const u32x4 x = load_vec<E>(px, c, rem), dy = load_vec<E>(pdy, c, rem);
         float w[V];
         load_param<W, V>(g.w, c, rem, 1.f, w);
+        float h[V];
+#pragma unroll
+        for (int j = 0; j < V; j++) h[j] = (E::get(x, j) - mean) * rstd;
+        // places past the row's end hold zeros, whose deviation may be infinite
+        if (rem < (uint32_t)V) {
+#pragma unroll
+            for (int j = 0; j < V; j++) h[j] = (uint32_t)j < rem ? h[j] : 0.f;
+        }
 #pragma unroll
         for (int j = 0; j < V; j++) {
             const float t = E::get(dy, j) * w[j];
-            s1 = fmaf(t, (E::get(x, j) - mean) * rstd, s1);
+            s1 = fmaf(t, h[j], s1);
             s2 += t;
         }
     }

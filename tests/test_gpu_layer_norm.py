@@ -443,3 +443,31 @@ def test_binding_refuses(S):
         S.spccl_layer_norm(x.half(), None, None, x.half())
     with pytest.raises(S.SpcclError):
         S.spccl_layer_norm_backward(x, x, w, one, one, None, w.clone(), w.clone(), None)     # no scratch
+
+
+@pytest.mark.parametrize("rows,cols,dtype", [(1, 65, "f32"), (3, 126, "f32"), (3, 126, "bf16"), (130, 1001, "bf16"),
+                                             (515, 64, "f32"), (515, 127, "f32"), (1031, 126, "bf16"), (1031, 1000, "bf16"),
+                                             (517, 1028, "f32"), (515, 16_386, "f32"), (1025, 16_388, "bf16"),
+                                             (1025, 3, "bf16")])
+@pytest.mark.parametrize("over", ["apart", "x", "dy"])
+def test_elements_that_do_not_exist_add_nothing(S, rows, cols, dtype, over):
+    """Constant rows far from zero: mean and rstd are finite, their product is
+    not, and no element deviates, so dweight is 0 and the rest finite.  Places
+    past a row's end and groups of lanes past the last row hold zeros, which do
+    deviate from that mean; they must not count."""
+    log(f"layer norm backward constant rows {rows}x{cols} {dtype} {over}")
+    x, dy = matrix(rows, cols, dtype, 1), matrix(rows, cols, dtype, 2)
+    x.fill_(2.0 ** 120)
+    w = vector(cols, "f32", 3, 0.3, 1.0)
+    mean = torch.full((rows,), 2.0 ** 120, device="cuda")
+    rstd = torch.full((rows,), 1e-5 ** -0.5, device="cuda")
+    assert not bool((mean * rstd).isfinite().any())
+    (ex, bx), (ew, bw), (eb, bb) = backward_bounds(dy, x, w, mean, rstd, dtype)
+    dx = {"apart": torch.empty_like(x), "x": x, "dy": dy}[over]
+    dw, db = torch.empty(cols, device="cuda"), torch.empty(cols, device="cuda")
+    scratch, _ = scratch_for(S, rows, cols)
+    S.spccl_layer_norm_backward(dy, x, w, mean, rstd, dx, dw, db, scratch)
+    torch.cuda.synchronize()
+    within(dx, ex, bx, "dx")
+    assert not bool(dw.any())
+    within(db, eb, bb + OUT["f32"] * eb.abs(), "dbias")
