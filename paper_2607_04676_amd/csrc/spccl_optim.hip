@@ -37,6 +37,13 @@ __device__ __forceinline__ uint32_t bf16_pair(float a, float b) {         // nea
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, bf16x2));
 }
 
+// A pair whose zeros have no sign: rounding made them of small negative values.
+__device__ __forceinline__ uint32_t no_minus_zero(uint32_t p) {
+    if ((p & 0x7FFFu) == 0) p &= 0xFFFF0000u;
+    if ((p & 0x7FFF0000u) == 0) p &= 0x0000FFFFu;
+    return p;
+}
+
 // A place in global memory, as a base that the whole block shares (scalar
 // registers) and a lane's offset in bytes.  A table's addresses are numbers to
 // the compiler; without the address space it would take generic accesses, which
@@ -174,13 +181,14 @@ __device__ __forceinline__ void prune_chunk(const PruneArgs& g, uint64_t e0, uin
 #pragma unroll
         for (int j = 0; j < 4; j++) {
             const float a = x[k].f[j] + g.leak * r[k].f[j];
-            const bool stays = fabsf(a) < tau || a == 0.f;      // a zero is absent, whatever its sign
+            // a zero is absent, whatever its sign (bf16's own zeros: below)
+            const bool stays = fabsf(a) < tau || a == 0.f;
             sent[j] = stays ? 0.f : a;
             back[j] = a;
         }
         u32x2 pairs;
         if constexpr (DT == kBF16) {
-            pairs = u32x2{bf16_pair(sent[0], sent[1]), bf16_pair(sent[2], sent[3])};
+            pairs = u32x2{no_minus_zero(bf16_pair(sent[0], sent[1])), no_minus_zero(bf16_pair(sent[2], sent[3]))};
 #pragma unroll
             for (int j = 0; j < 4; j++)
                 sent[j] = __uint_as_float(j & 1 ? pairs[j / 2] & 0xFFFF0000u : pairs[j / 2] << 16);

@@ -154,3 +154,44 @@ def test_binding_refuses(S):
             f()
     with pytest.raises(S.SpcclError):
         S.spccl_prune(x, x, tau, 1.0, x)
+
+
+@pytest.mark.parametrize("tau", [0.0, 1e-44, float("nan"), -1.0])
+@pytest.mark.parametrize("n", [40, 4096 * 3 + 5])
+def test_no_zero_is_sent_as_minus_zero(S, tau, n):
+    """A bf16 value that a sum below half the smallest one rounds to is a zero,
+    and a negative one has no sign either: the codec would count it as present.
+    The residual keeps the whole sum."""
+    log(f"prune minus zero tau={tau} n={n}")
+    unit = 2.0 ** -133                                          # bf16's smallest value
+    parts = np.array([0.5, 0.499, 0.25, 0.501, 0.75, 1.0, 1.5, 1e-4, 0.0, 40.0])
+    res = (np.resize(np.concatenate([-parts, parts]), n) * unit).astype(np.float32)
+    g, r = torch.zeros(n, dtype=torch.bfloat16, device="cuda"), torch.from_numpy(res).cuda()
+    S.spccl_prune(g, r, torch.tensor([tau], device="cuda"), 1.0, g)
+    torch.cuda.synchronize()
+    assert 0x8000 not in (g.view(torch.int16).cpu().numpy().view(np.uint16))
+    # to the nearest multiple of the smallest value, ties to even; what the
+    # threshold holds back is not sent
+    held = np.abs(res) < np.float32(tau)
+    sent = np.where(held, 0.0, np.rint(res.astype(np.float64) / unit) * unit)
+    assert np.array_equal(g.cpu().double().numpy(), sent)
+    assert np.array_equal(r.cpu().double().numpy(), res.astype(np.float64) - sent)
+    ws, msg = S.alloc_workspace(n, S.SPCCL_BF16), S.alloc_stream(n, S.SPCCL_BF16)
+    S.spccl_compress(g, msg, ws)
+    torch.cuda.synchronize()
+    assert S.spccl_read_header(msg)["nnz"] == np.count_nonzero(sent)
+
+
+def test_a_residual_that_fades_ends(S):
+    """Without new gradients and with a threshold of 0 a fading residual is sent
+    until it is too small for bf16; from then on nothing is."""
+    log("prune fading residual")
+    n = 10_000
+    rng = np.random.default_rng(5)
+    r = torch.from_numpy(rng.normal(0, 5e-4, n).astype(np.float32)).cuda()
+    g, tau = torch.zeros(n, dtype=torch.bfloat16, device="cuda"), torch.zeros(1, device="cuda")
+    out = torch.empty_like(g)
+    for k in range(40):
+        S.spccl_prune(g, r, tau, 0.9, out)
+        torch.cuda.synchronize()
+        assert 0x8000 not in (out.view(torch.int16).cpu().numpy().view(np.uint16)), k
