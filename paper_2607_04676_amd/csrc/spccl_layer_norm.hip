@@ -467,7 +467,7 @@ struct LnBackArgs {
     uint32_t cols;
 };
 
-constexpr uint32_t kBackThreads = 512;
+constexpr uint32_t kBackThreads = 512, kShortThreads = 512;
 __device__ const float kNoRow = 0.f;          // the mean and rstd of a group without a row
 
 // Each group of lanes walks over rows, keeping its columns' sums of dy h and
@@ -773,7 +773,7 @@ __global__ void __launch_bounds__(kSmallThreads) k_layer_norm_back_small(LnBackA
 }
 
 // Sums of dy h and dy over a strip of rows (grid y), a vector of columns per
-// thread: k_layer_norm_back's second result for long or very short rows.
+// thread: k_layer_norm_back's second result for long rows.
 template <class E>
 __global__ void __launch_bounds__(64) k_layer_norm_columns(LnBackArgs g) {
     constexpr int V = E::vec;
@@ -800,6 +800,50 @@ __global__ void __launch_bounds__(64) k_layer_norm_columns(LnBackArgs g) {
             part[j] = dw[j];
             part[g.cols + j] = db[j];
         }
+}
+
+// The same for rows shorter than a vector, of which there may be 2^31: a row
+// per thread and every 2^17th after it (256 blocks), so the chains of additions
+// stay short (64 strips of a lane each had 2^25 rows, and a sum of ones stopped
+// at 2^24); then the lanes, and the waves through LDS, in order.  70,000 x 5 bf16
+// with dx: 498 us, 1940 with the strips.
+template <class E>
+__global__ void __launch_bounds__(kShortThreads) k_layer_norm_columns_short(LnBackArgs g) {
+    constexpr int C = E::vec - 1;                                 // columns at most
+    constexpr uint32_t waves = kShortThreads / 64;
+    __shared__ float s_sum[2][waves][C];
+    float dw[C], db[C];
+#pragma unroll
+    for (int j = 0; j < C; j++) dw[j] = db[j] = 0.f;
+    const uint64_t step = (uint64_t)gridDim.x * kShortThreads;
+#pragma unroll 2
+    for (uint64_t row = (uint64_t)blockIdx.x * kShortThreads + threadIdx.x; row < g.rows; row += step) {
+        const u32x4 x = load_vec<E>(g.x + row * g.ldx, 0, g.cols), dy = load_vec<E>(g.dy + row * g.lddy, 0, g.cols);
+        const float mean = g.mean[row], rstd = g.rstd[row];
+#pragma unroll
+        for (int j = 0; j < C; j++) {
+            const float d = E::get(dy, j);
+            dw[j] = fmaf(d, (E::get(x, j) - mean) * rstd, dw[j]);
+            db[j] += d;
+        }
+    }
+    const uint32_t wave = threadIdx.x >> 6;
+#pragma unroll
+    for (int j = 0; j < C; j++) {
+        dw[j] = lanes_sum<64>(dw[j]);
+        db[j] = lanes_sum<64>(db[j]);
+        if ((threadIdx.x & 63u) == 0) {
+            s_sum[0][wave][j] = dw[j];
+            s_sum[1][wave][j] = db[j];
+        }
+    }
+    __syncthreads();
+    if (threadIdx.x >= 2 * g.cols) return;
+    const uint32_t which = threadIdx.x >= g.cols, c = threadIdx.x - which * g.cols;
+    float t = 0.f;
+#pragma unroll
+    for (uint32_t q = 0; q < waves; q++) t += s_sum[which][q][c];
+    g.part[(uint64_t)blockIdx.x * 2 * g.cols + threadIdx.x] = t;
 }
 
 // The weight's and the bias's gradient: the sums of `parts` blocks (at most
@@ -1004,6 +1048,11 @@ uint32_t back_blocks(uint64_t rows, uint32_t rows_per_block) {
     return (uint32_t)(b < kBackBlocks ? b : kBackBlocks);
 }
 uint32_t strips(uint64_t rows) { return (uint32_t)(rows < kStrips ? rows : kStrips); }
+// blocks of k_layer_norm_columns_short
+uint32_t short_blocks(uint64_t rows) {
+    const uint64_t b = (rows + kShortThreads - 1) / kShortThreads;
+    return (uint32_t)(b < kBackBlocks ? b : kBackBlocks);
+}
 
 // Backward passes of up to 1024 rows in bf16, 512 in fp32, are taken by
 // k_layer_norm_back_small at any width: reading their rows twice moves less
@@ -1020,7 +1069,8 @@ inline uint32_t small_strips(uint64_t rows) { return rows <= 128 ? 1 : (uint32_t
 template <class E>
 uint32_t back_parts(uint64_t rows, uint32_t cols) {
     if (small_backward<E>(rows)) return small_strips(rows);
-    if (cols > kMaxBackCols || cols < (uint32_t)E::vec) return strips(rows);
+    if (cols > kMaxBackCols) return strips(rows);
+    if (cols < (uint32_t)E::vec) return short_blocks(rows);
     return with_row<E, true>(cols, [&](auto l, auto waves, auto k) {
         return back_blocks(rows, Row<E, l(), waves(), k(), kBackThreads>::rows);
     });
@@ -1069,8 +1119,11 @@ spccl_status_t launch_backward(const LnBackArgs& g, int32_t gdtype, void* dw, vo
     if (g.cols > kMaxBackCols || g.cols < (uint32_t)E::vec) {
         // the columns' sums first: dx may be written over dy or x
         if (g.part) {
-            hipLaunchKernelGGL(k_layer_norm_columns<E>, dim3((g.cols + 64 * E::vec - 1) / (64 * E::vec), strips(g.rows)),
-                               dim3(64), 0, st, g);
+            if (g.cols < (uint32_t)E::vec)
+                hipLaunchKernelGGL(k_layer_norm_columns_short<E>, dim3(short_blocks(g.rows)), dim3(kShortThreads), 0, st, g);
+            else
+                hipLaunchKernelGGL(k_layer_norm_columns<E>,
+                                   dim3((g.cols + 64 * E::vec - 1) / (64 * E::vec), strips(g.rows)), dim3(64), 0, st, g);
             if (launch_status() != SPCCL_OK) return SPCCL_ERR_HIP;
         }
         if (g.dx) {

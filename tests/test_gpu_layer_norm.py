@@ -471,3 +471,55 @@ def test_elements_that_do_not_exist_add_nothing(S, rows, cols, dtype, over):
     within(dx, ex, bx, "dx")
     assert not bool(dw.any())
     within(db, eb, bb + OUT["f32"] * eb.abs(), "dbias")
+
+
+def short_rows_bounds(rows, dy, h):
+    """The columns' sums in 64 bits, and their bounds.  2^17 rows are worked on
+    at a time, so a lane adds rows / 2^17 terms one after another; lanes, waves
+    and blocks are joined in at most 56 steps, and h has 3 roundings."""
+    depth = 64 + rows // (1 << 17)
+    ew, eb = (dy * h).sum(0), dy.sum(0)
+    return (ew, depth * U * (dy * h).abs().sum(0) + TINY), (eb, depth * U * dy.abs().sum(0) + TINY)
+
+
+@pytest.mark.parametrize("rows", [513, 1025, 4099, 70_001, (1 << 17) + 1, (1 << 22) + 77])
+@pytest.mark.parametrize("dtype,cols", [("f32", 1), ("f32", 2), ("f32", 3), ("bf16", 1), ("bf16", 2), ("bf16", 5), ("bf16", 7)])
+@pytest.mark.parametrize("gdtype,accumulate", [("f32", False), ("f32", True), ("bf16", True)])
+def test_sums_over_short_rows(S, rows, dtype, cols, gdtype, accumulate):
+    """Gradients of the same sign in every row, where a long chain of additions
+    would round the same way again and again."""
+    log(f"layer norm backward short rows {rows}x{cols} {dtype} {gdtype} {accumulate}")
+    x, dy = matrix(rows, cols, dtype, 1, 0.3, 0.0, 1, 1), matrix(rows, cols, dtype, 2, 0.0, 0.1, 2)
+    mean, rstd = torch.full((rows,), -1.7, device="cuda"), torch.full((rows,), 0.7, device="cuda")
+    x[rows // 2:] = 0.3
+    h = (x.double() - mean.double()[:, None]) * rstd.double()[:, None]
+    (ew, bw), (eb, bb) = short_rows_bounds(rows, dy.double(), h)
+    dw, db = vector(cols, gdtype, 4, 10.0, 0.0), vector(cols, gdtype, 5, 10.0, 0.0)
+    if accumulate:
+        ew, eb = ew + dw.double(), eb + db.double()
+        bw, bb = bw + 2 * U * ew.abs(), bb + 2 * U * eb.abs()
+    scratch, whole = scratch_for(S, rows, cols)
+    again = dw.clone(), db.clone()
+    S.spccl_layer_norm_backward(dy, x, None, mean, rstd, None, dw, db, scratch, accumulate)
+    S.spccl_layer_norm_backward(dy, x, None, mean, rstd, None, *again, scratch, accumulate)
+    torch.cuda.synchronize()
+    within(dw, ew, bw + OUT[gdtype] * ew.abs(), "dweight")
+    within(db, eb, bb + OUT[gdtype] * eb.abs(), "dbias")
+    assert torch.equal(dw, again[0]) and torch.equal(db, again[1])
+    assert bool((whole[scratch.numel():] == 0xFF).all())
+
+
+def test_sums_over_the_most_rows(S):
+    """2^31 - 1 rows of one element: sums past 2^24, where fp32 no longer counts
+    in ones.  x and dy share their memory, and so do mean and rstd."""
+    log("layer norm backward of 2^31 - 1 rows")
+    rows = (1 << 31) - 1
+    x = torch.full((rows, 1), 1.5, dtype=torch.bfloat16, device="cuda")
+    one = torch.ones(rows, device="cuda")
+    dw, db = torch.empty(1, device="cuda"), torch.empty(1, device="cuda")
+    scratch, _ = scratch_for(S, rows, 1)
+    S.spccl_layer_norm_backward(x, x, None, one, one, None, dw, db, scratch)
+    torch.cuda.synchronize()
+    depth = 64 + rows // (1 << 17)
+    for got, each in ((dw, 0.75), (db, 1.5)):
+        assert abs(float(got) - each * rows) <= depth * U * each * rows
