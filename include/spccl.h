@@ -584,7 +584,9 @@ typedef struct {
     double beta1, beta2;     /* in [0, 1) */
     double eps;              /* >= 0 */
     uint64_t step;           /* t >= 1, for the bias corrections */
-    uint64_t seed;           /* of the stochastic rounding: give each step another */
+    uint64_t seed;           /* of the stochastic rounding: give each step another (its
+                                number will do), as the same one rounds every element
+                                the same way again and small changes never add up */
 } spccl_adamw_t;
 
 /* One step over a plan's tensors, one launch for those with ARRAY gradients

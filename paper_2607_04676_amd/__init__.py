@@ -625,13 +625,16 @@ def spccl_adamw_plan(tensors: list, table: torch.Tensor, stream=None) -> spccl_a
 
 
 def spccl_adamw_step(plan: spccl_adamw_plan_t, ws: torch.Tensor, lr: float, beta1: float = 0.9, beta2: float = 0.999,
-                     eps: float = 1e-8, step: int = 1, seed: int = 0, grad_scale: torch.Tensor | None = None,
+                     eps: float = 1e-8, step: int = 1, seed: int | None = None, grad_scale: torch.Tensor | None = None,
                      stream=None) -> None:
     """One AdamW step over the plan's tensors; gradients are multiplied by
-    grad_scale (one fp32 on the device) first."""
+    grad_scale (one fp32 on the device) first.  seed: of the stochastic rounding
+    of 8-bit moments and bf16 parameters, another for each step, or rounding the
+    same way each time holds small changes back; the step's number if none is
+    given."""
     if grad_scale is not None and (grad_scale.numel() != 1 or grad_scale.dtype != torch.float32):
         raise ValueError("spccl_adamw_step: grad_scale is one fp32")
-    h = spccl_adamw_t(lr, beta1, beta2, eps, step, seed)
+    h = spccl_adamw_t(lr, beta1, beta2, eps, step, step if seed is None else seed)
     _check(_lib.spccl_adamw_step(ctypes.byref(plan), ctypes.byref(h), _ptr_or_null(grad_scale), ws.data_ptr(),
                                  _nbytes(ws), _stream(stream)), "spccl_adamw_step")
 

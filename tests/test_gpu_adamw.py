@@ -607,3 +607,41 @@ def test_a_shared_gradient(S):
     for a, b in zip(sets[0] + sets[1], sets[2] + sets[3]):
         assert torch.equal(a, b)
     assert float(sets[0][0][0]) < 1.0
+
+
+def test_a_second_moment_follows_its_decay_with_the_default_seed(S):
+    """A caller who gives no seed but counts the steps: a second moment without
+    gradients falls as beta2^t.  A step's rounding is unbiased and off by at
+    most one spacing q <= v / 8, a deviation of at most v / 16; over T steps of
+    N elements the mean's is at most v sqrt(T) / 16 / sqrt(N).  6 of them, the
+    random bits' resolution (2^-20 q a step) and the products' own roundings
+    (2 u a step) are allowed."""
+    log("adamw default seed")
+    n, steps, b2 = 1 << 16, 1000, 0.999
+    p, g = torch.zeros(n, device="cuda"), torch.zeros(n, device="cuda")
+    state = S.alloc_adamw_state(n, S.SPCCL_STATE_F8)
+    state["v"].view(torch.uint8).fill_(0x70)                    # 2^7, the lowest a block's largest may be
+    state["v_scale"].view(torch.uint8).fill_(122)               # 2^-5: v = 4
+    tensors = [S.adamw_tensor(p, g, **state)]
+    plan = S.spccl_adamw_plan(tensors, torch.empty(S.spccl_adamw_plan_bytes(tensors), dtype=torch.uint8, device="cuda"))
+    ws = torch.zeros(256, dtype=torch.uint8, device="cuda")
+    for t in range(1, steps + 1):
+        S.spccl_adamw_step(plan, ws, 1e-3, 0.9, b2, step=t)
+    torch.cuda.synchronize()
+    v = decode(state["v"].view(torch.uint8).cpu().numpy(), state["v_scale"].view(torch.uint8).cpu().numpy())
+    exact = 4.0 * float(f32(b2)) ** steps
+    tol = exact * (6 * np.sqrt(steps) / 16 / np.sqrt(n) + steps * (2.0 ** -23 + 2 * U))
+    assert abs(v.astype(np.float64).mean() - exact) <= tol
+
+
+def test_the_default_seed_is_the_step(S):
+    """No seed: the step's number.  A seed that is given is taken as it is, 0 too."""
+    log("adamw seed given")
+    got = []
+    for kw in (dict(step=5), dict(step=5, seed=5), dict(step=5, seed=0), dict(step=5, seed=None)):
+        c = Case(S, [4096], "bf16", "f32", 8, "array", 3)
+        S.spccl_adamw_step(c.plan, c.ws, 1e-3, **kw)
+        torch.cuda.synchronize()
+        got.append(c.read()[0])
+    same = lambda a, b: all(np.array_equal(a[k], b[k]) for k in a)  # noqa: E731
+    assert same(got[0], got[1]) and same(got[0], got[3]) and not same(got[0], got[2])
