@@ -523,3 +523,169 @@ def test_sums_over_the_most_rows(S):
     depth = 64 + rows // (1 << 17)
     for got, each in ((dw, 0.75), (db, 1.5)):
         assert abs(float(got) - each * rows) <= depth * U * each * rows
+
+
+# Widths in every layout of the backward kernel that keeps its rows in registers
+# (whole vectors, an odd length, and the widest), and one past the last; rows past
+# the few that another kernel takes, and no multiple of what a block holds.
+BACK_WIDTHS = [8, 63, 64, 71, 128, 200, 251, 256, 333, 512, 777, 1024, 1111, 1536, 1544, 1999, 2048, 2056, 2500, 3001, 4095, 4096,
+               4104, 5001, 6144, 6145, 7000, 8192, 8200, 9999, 12_288, 12_289, 14_336, 16_383, 16_384, 16_385, 16_392]
+
+
+@pytest.mark.parametrize("cols", BACK_WIDTHS)
+@pytest.mark.parametrize("dtype,rows,wdtype,gdtype,accumulate",
+                         [("f32", 519, "f32", "f32", False), ("f32", 1031, "bf16", "f32", True),
+                          ("bf16", 1031, "f32", "f32", False), ("bf16", 2063, "bf16", "bf16", True)])
+@pytest.mark.parametrize("place", ["aligned", "odd pitch", "late"])
+def test_backward_in_every_layout(S, cols, dtype, rows, wdtype, gdtype, accumulate, place):
+    """Values apart and over x and over dy, from rows that start on 16 bytes and
+    from rows that do not."""
+    log(f"layer norm backward layouts {rows}x{cols} {dtype} {wdtype} {gdtype} {accumulate} {place}")
+    vec = 4 if dtype == "f32" else 8
+    # "aligned": every row starts on 16 bytes, whatever its length
+    pad, offset = {"aligned": (-cols % vec, 0), "odd pitch": (1 - cols % 2 + 2, 0), "late": (-cols % vec, 1)}[place]
+    x, dy = matrix(rows, cols, dtype, cols, 2.0, 0.7, pad, offset), matrix(rows, cols, dtype, cols + 1, 1.0, 0.1, pad, offset)
+    w = vector(cols, wdtype, 3, 0.3, 1.0)
+    mean = x.float().mean(1)
+    rstd = 1.0 / (x.float().var(1, unbiased=False) + 1e-5).sqrt()
+    dw0, db0 = vector(cols, gdtype, 4, 1.0, 0.0), vector(cols, gdtype, 5, 1.0, 0.0)
+    (ex, bx), (ew, bw), (eb, bb) = backward_bounds(dy, x, w, mean, rstd, dtype)
+    if accumulate:
+        ew, eb = ew + dw0.double(), eb + db0.double()
+        bw, bb = bw + 2 * U * ew.abs(), bb + 2 * U * eb.abs()
+    scratch, whole = scratch_for(S, rows, cols)
+    first = None
+    for over in ("apart", "x", "dy"):
+        a, b = (matrix(rows, cols, dtype, 1, 0.0, 0.0, pad, offset).copy_(t) for t in (dy, x))
+        dx = {"apart": matrix(rows, cols, dtype, 6, 1.0, 0.0, pad, offset), "x": b, "dy": a}[over]
+        dw, db = dw0.clone(), db0.clone()
+        S.spccl_layer_norm_backward(a, b, w, mean, rstd, dx, dw, db, scratch, accumulate)
+        torch.cuda.synchronize()
+        if first is None:
+            within(dx, ex, bx, "dx")
+            within(dw, ew, bw + OUT[gdtype] * ew.abs(), "dweight")
+            within(db, eb, bb + OUT[gdtype] * eb.abs(), "dbias")
+            first = dx.clone(), dw, db
+        assert all(torch.equal(p, q) for p, q in zip(first, (dx, dw, db)))
+        assert untouched(a) and untouched(b) and untouched(dx)
+    assert bool((whole[scratch.numel():] == 0xFF).all())
+
+
+@pytest.mark.parametrize("cols", [64, 63, 1000, 1600, 2048, 3001, 4096, 6000, 8192, 8195, 12_000, 16_384, 16_390])
+@pytest.mark.parametrize("dtype,rows", [("f32", 519), ("f32", 4099), ("bf16", 1031), ("bf16", 4099)])
+@pytest.mark.parametrize("over", ["x", "dy", "apart"])
+def test_a_nan_gradient_stays_in_its_row_and_column_of_many(S, dtype, rows, cols, over):
+    """The first and the last row, past the few rows that another kernel takes."""
+    log(f"layer norm backward nan {rows}x{cols} {dtype} {over}")
+    x, dy = matrix(rows, cols, dtype, 1, 2.0, 0.5), matrix(rows, cols, dtype, 2)
+    mean = x.float().mean(1)
+    rstd = 1.0 / (x.float().var(1, unbiased=False) + 1e-5).sqrt()
+    dy[rows - 1, 5] = float("nan")
+    dy[0, cols - 1] = float("nan")
+    dx = {"x": x, "dy": dy, "apart": torch.empty_like(x)}[over]
+    dw, db = torch.empty(cols, device="cuda"), torch.empty(cols, device="cuda")
+    scratch, _ = scratch_for(S, rows, cols)
+    S.spccl_layer_norm_backward(dy, x, None, mean, rstd, dx, dw, db, scratch)
+    torch.cuda.synchronize()
+    assert bool(dx[1:rows - 1].isfinite().all()) and bool(dx[0].isnan().all()) and bool(dx[rows - 1].isnan().all())
+    for g in (dw, db):
+        assert g.isnan().nonzero().flatten().tolist() == [5, cols - 1]
+
+
+@pytest.mark.parametrize("rows,cols,dtype", [(1100, 1600, "bf16"), (1100, 4096, "bf16"), (600, 8192, "f32"), (600, 13_000, "f32"),
+                                             (600, 17_000, "f32")])
+def test_backward_parts_of_many_rows(S, rows, cols, dtype):
+    """Each gradient alone equals the same gradient of the whole call."""
+    log(f"layer norm backward parts {rows}x{cols} {dtype}")
+    x, dy = matrix(rows, cols, dtype, 1, 2.0, 0.5), matrix(rows, cols, dtype, 2)
+    w = vector(cols, "f32", 3, 0.3, 1.0)
+    mean = x.float().mean(1)
+    rstd = 1.0 / (x.float().var(1, unbiased=False) + 1e-5).sqrt()
+    new = lambda: (torch.empty_like(x), torch.empty(cols, device="cuda"), torch.empty(cols, device="cuda"))  # noqa: E731
+    whole = new()
+    scratch, _ = scratch_for(S, rows, cols)
+    S.spccl_layer_norm_backward(dy, x, w, mean, rstd, *whole, scratch)
+    for wanted in ((1, 0, 0), (0, 1, 1), (0, 1, 0), (0, 0, 1), (1, 1, 0), (1, 0, 1)):
+        part = [t if k else None for t, k in zip(new(), wanted)]
+        S.spccl_layer_norm_backward(dy, x, w, mean, rstd, *part, scratch if any(wanted[1:]) else None)
+        torch.cuda.synchronize()
+        for got, exp in zip(part, whole):
+            assert got is None or torch.equal(got, exp), wanted
+
+
+@pytest.mark.parametrize("cols", [300, 1600, 5000])
+def test_many_rows_past_32_bit_offsets(S, cols):
+    """Rows whose offsets pass 32 bits in elements and bytes, in the kernel that
+    many rows take, also over x."""
+    log(f"layer norm backward far rows of many {cols}")
+    rows, pitch = 1100, 1 << 21
+    buf = torch.empty((rows - 1) * pitch + cols, dtype=torch.bfloat16, device="cuda")
+    x = buf.as_strided((rows, cols), (pitch, 1))
+    x.copy_(matrix(rows, cols, "bf16", 3, 2.0, 0.5))
+    dy = matrix(rows, cols, "bf16", 4)
+    mean = x.float().mean(1)
+    rstd = 1.0 / (x.float().var(1, unbiased=False) + 1e-5).sqrt()
+    (ex, bx), (ew, bw), (eb, bb) = backward_bounds(dy, x, None, mean, rstd, "bf16")
+    dw, db = torch.empty(cols, device="cuda"), torch.empty(cols, device="cuda")
+    scratch, _ = scratch_for(S, rows, cols)
+    S.spccl_layer_norm_backward(dy, x, None, mean, rstd, x, dw, db, scratch)
+    torch.cuda.synchronize()
+    within(x, ex, bx, "dx")
+    within(dw, ew, bw + OUT["f32"] * ew.abs(), "dweight")
+    within(db, eb, bb + OUT["f32"] * eb.abs(), "dbias")
+
+
+@pytest.mark.parametrize("rows,cols,dtype", [(1100, 1600, "bf16"), (1100, 8192, "bf16"), (600, 13_000, "f32"), (3000, 5, "bf16"),
+                                             (600, 17_000, "f32")])
+def test_backward_of_many_rows_in_a_graph(S, rows, cols, dtype):
+    log(f"layer norm backward graph {rows}x{cols} {dtype}")
+    x, dy = matrix(rows, cols, dtype, 1, 2.0, 0.5), matrix(rows, cols, dtype, 2)
+    w = vector(cols, "f32", 3, 0.3, 1.0)
+    mean, rstd = torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+    new = lambda: (torch.empty_like(x), torch.empty(cols, device="cuda"), torch.empty(cols, device="cuda"))  # noqa: E731
+    scratch, _ = scratch_for(S, rows, cols)
+
+    def both(o):
+        S.spccl_layer_norm(x, w, None, o[0], mean, rstd)
+        S.spccl_layer_norm_backward(dy, x, w, mean, rstd, *o, scratch)
+
+    out = new()
+    both(out)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        both(out)
+    for k in range(4):
+        x.mul_(1.01)
+        dy.add_(0.01)
+        for t in out:
+            t.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        eager = new()
+        both(eager)
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, q) for p, q in zip(out, eager)), k
+
+
+@pytest.mark.parametrize("cols", [8, 71, 200, 251, 256, 333, 777, 1032, 1111, 1536, 1544, 2056, 3001, 3080, 5000, 6144, 6152, 9999,
+                                  10_240, 10_248, 11_111, 12_288, 12_296, 14_001, 20_000, 24_576, 24_584, 30_001])
+@pytest.mark.parametrize("dtype,wdtype", [("f32", "f32"), ("f32", "bf16"), ("bf16", "bf16"), ("bf16", "f32")])
+def test_forward_in_every_layout(S, cols, dtype, wdtype):
+    """The widths between the steps of the sizes above; over x too."""
+    log(f"layer norm layouts {cols} {dtype} {wdtype}")
+    rows = 19
+    for pad, offset in ((-cols % 8, 0), (3, 1)):
+        x = matrix(rows, cols, dtype, cols, 2.0, 0.7, pad, offset)
+        y = matrix(rows, cols, dtype, 1, 1.0, 0.0, pad, offset)
+        w, b = vector(cols, wdtype, 2, 0.3, 1.0), vector(cols, wdtype, 3, 0.3, 0.1)
+        mean, rstd = torch.full((rows,), 9.0, device="cuda"), torch.full((rows,), 9.0, device="cuda")
+        S.spccl_layer_norm(x, w, b, y, mean, rstd, 1e-5)
+        torch.cuda.synchronize()
+        (m, em), (r, er), (e, ee) = forward_bounds(x, w, b, 1e-5, dtype)
+        within(mean[:, None], m, em, "mean")
+        within(rstd[:, None], r, er, "rstd")
+        within(y, e, ee, "y")
+        S.spccl_layer_norm(x, w, b, x, None, None, 1e-5)
+        torch.cuda.synchronize()
+        assert torch.equal(x, y) and untouched(x) and untouched(y)
