@@ -538,6 +538,13 @@ def spccl_layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: torch.T
 
 # ---- pruning and AdamW ---------------------------------------------------------------
 
+def _device_value(t: torch.Tensor, what: str) -> None:
+    """A single value that kernels read: one in pageable host memory, as
+    torch.tensor makes it without a device, would fault there."""
+    if t.numel() != 1 or t.dtype != torch.float32 or not (t.is_cuda or t.is_pinned()):
+        raise ValueError(f"{what} is one fp32 in device memory, got {tuple(t.shape)} {t.dtype} on {t.device}")
+
+
 def spccl_prune(grad: torch.Tensor, residual: torch.Tensor, threshold: torch.Tensor, leak: float, out: torch.Tensor,
                 stream=None) -> None:
     """Split grad + leak * residual: what reaches the threshold (a device value)
@@ -545,9 +552,9 @@ def spccl_prune(grad: torch.Tensor, residual: torch.Tensor, threshold: torch.Ten
     n = grad.numel()
     if not (grad.is_contiguous() and residual.is_contiguous() and out.is_contiguous()):
         raise ValueError("spccl_prune: contiguous tensors are needed")
-    if residual.numel() != n or out.numel() != n or out.dtype != grad.dtype or residual.dtype != torch.float32 \
-            or threshold.numel() != 1 or threshold.dtype != torch.float32:
-        raise ValueError("spccl_prune: residual (fp32) and out (grad's dtype) hold grad's elements, threshold one fp32")
+    if residual.numel() != n or out.numel() != n or out.dtype != grad.dtype or residual.dtype != torch.float32:
+        raise ValueError("spccl_prune: residual (fp32) and out (grad's dtype) hold grad's elements")
+    _device_value(threshold, "spccl_prune: threshold")
     _check(_lib.spccl_prune(grad.data_ptr(), residual.data_ptr(), threshold.data_ptr(), float(leak), out.data_ptr(), n,
                             _dt(grad), _stream(stream)), "spccl_prune")
 
@@ -632,8 +639,8 @@ def spccl_adamw_step(plan: spccl_adamw_plan_t, ws: torch.Tensor, lr: float, beta
     of 8-bit moments and bf16 parameters, another for each step, or rounding the
     same way each time holds small changes back; the step's number if none is
     given."""
-    if grad_scale is not None and (grad_scale.numel() != 1 or grad_scale.dtype != torch.float32):
-        raise ValueError("spccl_adamw_step: grad_scale is one fp32")
+    if grad_scale is not None:
+        _device_value(grad_scale, "spccl_adamw_step: grad_scale")
     h = spccl_adamw_t(lr, beta1, beta2, eps, step, step if seed is None else seed)
     _check(_lib.spccl_adamw_step(ctypes.byref(plan), ctypes.byref(h), _ptr_or_null(grad_scale), ws.data_ptr(),
                                  _nbytes(ws), _stream(stream)), "spccl_adamw_step")

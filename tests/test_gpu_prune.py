@@ -195,3 +195,17 @@ def test_a_residual_that_fades_ends(S):
         S.spccl_prune(g, r, tau, 0.9, out)
         torch.cuda.synchronize()
         assert 0x8000 not in (out.view(torch.int16).cpu().numpy().view(np.uint16)), k
+
+
+def test_a_threshold_in_pinned_memory(S):
+    """Kernels read pinned host memory too; pageable memory is refused."""
+    log("prune pinned threshold")
+    x = torch.linspace(-1, 1, 100, device="cuda")
+    r, out = torch.zeros(100, device="cuda"), torch.empty(100, device="cuda")
+    tau = torch.empty(1, pin_memory=True)
+    tau[0] = 0.5
+    S.spccl_prune(x, r, tau, 1.0, out)
+    torch.cuda.synchronize()
+    assert torch.equal(out, torch.where(x.abs() >= 0.5, x, 0.0))
+    with pytest.raises(ValueError):
+        S.spccl_prune(x, r, torch.tensor([0.5]), 1.0, out)

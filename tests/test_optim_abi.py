@@ -117,3 +117,14 @@ def test_step_refusals(S):
         d = dict(lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, step=1, seed=0)
         d.update(bad)
         assert step(empty, S.spccl_adamw_t(**d)) == INVALID, bad
+
+
+def test_values_in_host_memory(S):
+    """A threshold or a scale that kernels could not read is refused by the
+    binding, before the call."""
+    torch = pytest.importorskip("torch")
+    x, value = torch.zeros(8), torch.tensor([0.5])
+    with pytest.raises(ValueError, match="threshold"):
+        S.spccl_prune(x, x.clone(), value, 1.0, x.clone())
+    with pytest.raises(ValueError, match="grad_scale"):
+        S.spccl_adamw_step(S.spccl_adamw_plan_t(), torch.zeros(256, dtype=torch.uint8), 1e-3, grad_scale=value)
