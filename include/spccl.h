@@ -602,7 +602,10 @@ typedef struct {
  * equal bits.  A step captured into a HIP graph replays with the values of
  * `hyper` at its capture.  ws: at least the 256-byte control block of a workspace; a
  * message that fails its header checks sets SPCCL_ERR_CORRUPT_STREAM there and
- * its tensors are not changed; a tile that fails its checks counts as empty. */
+ * its tensors are not changed; a tile that fails its checks counts as empty.
+ * grad_scale and ws must lie outside everything the step writes and outside the
+ * plan's table: the call refuses a ws in the table, and has the tensors'
+ * addresses only in device memory to check the rest by. */
 spccl_status_t spccl_adamw_step(const spccl_adamw_plan_t* plan, const spccl_adamw_t* hyper, const float* grad_scale,
                                 void* ws, uint64_t ws_bytes, void* stream);
 

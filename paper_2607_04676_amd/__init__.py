@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+from bisect import bisect_left
 
 import torch
 
@@ -31,6 +32,7 @@ SPCCL_ARRAY, SPCCL_STREAM = 0, 1
 SPCCL_STATE_F32, SPCCL_STATE_F8 = 0, 1
 SPCCL_STATE_BLOCK = 32
 HEADER_BYTES = 48
+CONTROL_BYTES = 256
 NNZ_UNKNOWN = (1 << 64) - 1
 
 # every symbol the C header declares
@@ -84,6 +86,7 @@ class spccl_adamw_plan_t(ctypes.Structure):
     _fields_ = [("magic", ctypes.c_uint32), ("param_dtype", ctypes.c_int32), ("grad_dtype", ctypes.c_int32),
                 ("state", ctypes.c_int32), ("count", ctypes.c_int32), ("pad", ctypes.c_int32),
                 ("array_chunks", ctypes.c_uint64), ("stream_chunks", ctypes.c_uint64), ("table", ctypes.c_void_p)]
+    _written = ((), ())       # the starts and the ends of what a step writes
 
 
 class spccl_adamw_t(ctypes.Structure):
@@ -628,7 +631,27 @@ def spccl_adamw_plan(tensors: list, table: torch.Tensor, stream=None) -> spccl_a
                                  table.data_ptr(), _nbytes(table), ctypes.byref(plan), _stream(stream)),
            "spccl_adamw_plan")
     plan._tensors = (list(tensors), table)
+    plan._written = _written(tensors, pdt, state)
     return plan
+
+
+def _written(tensors: list, pdt: int, state: int) -> tuple:
+    """The starts and the ends of what a step writes, in order (the plan has
+    refused overlaps among them)."""
+    p, s = (4 if pdt == SPCCL_F32 else 2), (4 if state == SPCCL_STATE_F32 else 1)
+    spans = []
+    for t in tensors:
+        blocks = -(-t.n // SPCCL_STATE_BLOCK)
+        spans += [(a, a + b) for a, b in ((t.param, p * t.n), (t.model, 2 * t.n), (t.m, s * t.n), (t.v, s * t.n),
+                                          (t.m_scale, blocks), (t.v_scale, blocks)) if a and b]
+    spans.sort()
+    return [a for a, _ in spans], [b for _, b in spans]
+
+
+def _meets(written: tuple, at: int, nbytes: int) -> bool:
+    """Whether nbytes from an address on share a byte with the written spans."""
+    k = bisect_left(written[0], at + nbytes)
+    return k > 0 and written[1][k - 1] > at
 
 
 def spccl_adamw_step(plan: spccl_adamw_plan_t, ws: torch.Tensor, lr: float, beta1: float = 0.9, beta2: float = 0.999,
@@ -639,11 +662,17 @@ def spccl_adamw_step(plan: spccl_adamw_plan_t, ws: torch.Tensor, lr: float, beta
     of 8-bit moments and bf16 parameters, another for each step, or rounding the
     same way each time holds small changes back; the step's number if none is
     given."""
+    written, at, scale = plan._written, ws.data_ptr(), None
     if grad_scale is not None:
         _device_value(grad_scale, "spccl_adamw_step: grad_scale")
+        scale = grad_scale.data_ptr()
+        if _meets(written, scale, 4):
+            raise ValueError("spccl_adamw_step: grad_scale overlaps what the step writes")
+    if _meets(written, at, CONTROL_BYTES):
+        raise ValueError("spccl_adamw_step: the workspace's control block overlaps what the step writes")
     h = spccl_adamw_t(lr, beta1, beta2, eps, step, step if seed is None else seed)
-    _check(_lib.spccl_adamw_step(ctypes.byref(plan), ctypes.byref(h), _ptr_or_null(grad_scale), ws.data_ptr(),
-                                 _nbytes(ws), _stream(stream)), "spccl_adamw_step")
+    _check(_lib.spccl_adamw_step(ctypes.byref(plan), ctypes.byref(h), scale, at, ws.nbytes, _stream(stream)),
+           "spccl_adamw_step")
 
 
 # ---- tensor helpers (allocation stays with the caller; these only size buffers) -----

@@ -573,10 +573,13 @@ uint64_t chunks_of(const spccl_adamw_tensor_t& t) {
     return (lead + t.n + chunk - 1) / chunk;
 }
 
+uint64_t table_bytes(int32_t count, uint64_t chunks) {
+    return (uint64_t)count * sizeof(AdamTensor) + (chunks * 4 + 15) / 16 * 16;
+}
 uint64_t table_bytes(const spccl_adamw_tensor_t* t, int32_t count, uint64_t* arrays, uint64_t* streams) {
     *arrays = *streams = 0;
     for (int32_t i = 0; i < count; i++) (is_stream(t[i]) ? *streams : *arrays) += chunks_of(t[i]);
-    return (uint64_t)count * sizeof(AdamTensor) + ((*arrays + *streams) * 4 + 15) / 16 * 16;
+    return table_bytes(count, *arrays + *streams);
 }
 
 spccl_status_t check_tensor(const spccl_adamw_tensor_t& t, int32_t pdt, int32_t gdt, int32_t state) {
@@ -762,6 +765,8 @@ spccl_status_t spccl_adamw_step(const spccl_adamw_plan_t* plan, const spccl_adam
         return SPCCL_ERR_INVALID_ARG;
     if (!aligned_to(grad_scale, 4) || !ws || !aligned_to(ws, 16)) return SPCCL_ERR_INVALID_ARG;
     if (ws_bytes < sizeof(WsCtrl)) return SPCCL_ERR_WORKSPACE;
+    const uint64_t table = table_bytes(plan->count, plan->array_chunks + plan->stream_chunks);
+    if (overlaps(ws, sizeof(WsCtrl), plan->table, table)) return SPCCL_ERR_INVALID_ARG;
     const double t = (double)h.step;
     AdamArgs a{};
     a.table = static_cast<const AdamTensor*>(plan->table);

@@ -645,3 +645,36 @@ def test_the_default_seed_is_the_step(S):
         got.append(c.read()[0])
     same = lambda a, b: all(np.array_equal(a[k], b[k]) for k in a)  # noqa: E731
     assert same(got[0], got[1]) and same(got[0], got[3]) and not same(got[0], got[2])
+
+
+@pytest.mark.parametrize("state", [32, 8])
+def test_a_scale_or_a_workspace_that_the_step_writes_over(S, state):
+    """The step refuses them and changes nothing; their neighbours are taken."""
+    log(f"adamw overlaps of the step {state}")
+    c = Case(S, [1000, 0, 200], "f32", "f32", state, "array", 3, copy=True)
+    before = c.read()
+    lr, b1, b2, eps, t = HYPER
+    step = lambda **kw: S.spccl_adamw_step(c.plan, kw.pop("ws", c.ws), lr, b1, b2, eps, t, 1, **kw)  # noqa: E731
+    inside = [v[i].view(torch.uint8) for v in c.views.values() for i in (0, 2)]
+    for b in inside:
+        for at in (0, (b.numel() - 4) // 4 * 4):
+            if (b.data_ptr() + at) % 4 == 0 and at + 4 <= b.numel():
+                with pytest.raises(ValueError, match="grad_scale"):
+                    step(grad_scale=b[at:at + 4].view(torch.float32))
+    p = c.buffers["param"].view(torch.uint8)
+    for at in (0, 3776, 3840):                                   # the first 1000 elements end at 4000
+        with pytest.raises(ValueError, match="workspace"):
+            step(ws=p[at:at + 256])
+    table = c.plan._tensors[1]
+    for at in (0, table.numel() // 16 * 16 - 256):
+        with pytest.raises(S.SpcclError):
+            step(ws=table[at:at + 256])
+    torch.cuda.synchronize()
+    for b, a in zip(before, c.read()):
+        assert all(np.array_equal(b[k].view(np.uint8), a[k].view(np.uint8)) for k in b)
+    # a scale right behind a tensor
+    c.untouched = {k: t.clone() for k, t in c.buffers.items()}
+    c.buffers["param"][1000] = c.untouched["param"][1000] = 0.37
+    step(grad_scale=c.buffers["param"][1000:1001])
+    torch.cuda.synchronize()
+    c.check(c.read(), c.expect(before, HYPER, 1, f32(0.37)))
