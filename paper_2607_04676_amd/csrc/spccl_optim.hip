@@ -330,7 +330,7 @@ __device__ __forceinline__ uint32_t encode4(const float* x, float up, uint32_t h
     return (uint32_t)word;
 }
 __device__ __forceinline__ Quad decode4(uint32_t word, uint32_t scale) {
-    const float s = __uint_as_float(scale << 23);
+    const float s = __uint_as_float(scale == 255u ? 0x7FC00000u : scale << 23);    // 255: NaN, whatever the values
     const auto a = __builtin_amdgcn_cvt_pk_f32_fp8((int)word, false);
     const auto b = __builtin_amdgcn_cvt_pk_f32_fp8((int)word, true);
     return Quad{{a[0] * s, a[1] * s, b[0] * s, b[1] * s}};

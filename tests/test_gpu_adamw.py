@@ -678,3 +678,25 @@ def test_a_scale_or_a_workspace_that_the_step_writes_over(S, state):
     step(grad_scale=c.buffers["param"][1000:1001])
     torch.cuda.synchronize()
     c.check(c.read(), c.expect(before, HYPER, 1, f32(0.37)))
+
+
+@pytest.mark.parametrize("which", ["m", "v"])
+def test_a_block_of_scale_255_is_nan_whatever_its_values(S, which):
+    """8-bit moments that another program wrote: a scale of 255 stands for NaN, so
+    its block's parameters become NaN and its scale stays; no other block changes."""
+    log(f"adamw scale 255 {which}")
+    c, clean = (Case(S, [1000], "f32", "f32", 8, "array", 12) for _ in range(2))
+    codes, scales = c.views[which][0], c.views[which + "_scale"][0]
+    codes[64:96] = torch.arange(32, dtype=torch.uint8, device="cuda") * 4     # 0 and ordinary values
+    scales[2] = 255
+    for x in (c, clean):
+        x.step(HYPER, 3)
+    got, ref = c.read()[0], clean.read()[0]
+    assert np.isnan(got["param"][64:96]).all()
+    assert got[which + "_scale"][2] == 255 and (got[which + "_scale"] == 255).sum() == 1
+    assert np.isnan(decode(got[which], got[which + "_scale"])[64:96]).all()
+    for k in got:
+        per = 32 if k.endswith("_scale") else 1
+        other = np.ones(got[k].size, bool)
+        other[64 // per:96 // per] = False
+        assert np.array_equal(got[k][other], ref[k][other]), k
