@@ -513,8 +513,8 @@ spccl_status_t spccl_layer_norm_backward(const void* dy, uint64_t lddy, const vo
  *   a = grad + leak * residual         (fp32, each operation rounded)
  *   out = a rounded to dtype where |a| >= *threshold, +0.0 elsewhere
  *   residual = a - out
- * so what is not sent now is added to a later gradient (leak = 1; below 1 old
- * residuals fade), and in bf16 the sent values' rounding errors as well.  The
+ * so what is not sent now is added to a later gradient (leak in [0, 1]: below 1
+ * old residuals fade), and in bf16 the sent values' rounding errors as well.  The
  * result is what the codec and the collectives take.  grad and out have
  * `dtype`; out may be grad itself; residual is fp32.  threshold: a device
  * value, e.g. a quantile of a sample of |a|.  A NaN, an infinity, or a value

@@ -641,9 +641,16 @@ def _written(tensors: list, pdt: int, state: int) -> tuple:
     p, s = (4 if pdt == SPCCL_F32 else 2), (4 if state == SPCCL_STATE_F32 else 1)
     spans = []
     for t in tensors:
-        blocks = -(-t.n // SPCCL_STATE_BLOCK)
-        spans += [(a, a + b) for a, b in ((t.param, p * t.n), (t.model, 2 * t.n), (t.m, s * t.n), (t.v, s * t.n),
-                                          (t.m_scale, blocks), (t.v_scale, blocks)) if a and b]
+        n, model = t.n, t.model
+        if not n:
+            continue
+        for a, size in ((t.param, p * n), (t.m, s * n), (t.v, s * n)):
+            spans.append((a, a + size))
+        if model:
+            spans.append((model, model + 2 * n))
+        if state == SPCCL_STATE_F8:
+            for a in (t.m_scale, t.v_scale):
+                spans.append((a, a + -(-n // SPCCL_STATE_BLOCK)))
     spans.sort()
     return [a for a, _ in spans], [b for _, b in spans]
 

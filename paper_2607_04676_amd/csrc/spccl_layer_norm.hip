@@ -1059,7 +1059,11 @@ uint32_t short_blocks(uint64_t rows) {
 // than a pair of sums per column and CU (us with the host's part, so / by
 // k_layer_norm_back, bf16: 64 x 1024 9.7 / 12.9, 256 x 8192 12.3 / 17.1, 512 x
 // 16384 22 / 40, 1024 x 8192 19 / 26, 1536 x 16384 60 / 55; fp32: 512 x 4096
-// 12.1 / 13.2, 1024 x 4096 18.6 / 16.5).  Strips of 64 rows beyond 128.
+// 12.1 / 13.2, 1024 x 4096 18.6 / 16.5).  Narrow rows leave most lanes of its
+// blocks idle and are much the same either way (the kernels alone, 256 x 256 bf16
+// 7.6 / 9.0, 256 x 128 8.1 / 7.1, 256 x 64 8.1 / 7.4; fp32 6.0 / 9.4, 6.5 / 6.6,
+// 6.4 / 7.1); a call of 129 rows and more takes 11-12 with either.  Strips of 64
+// rows beyond 128.
 template <class E>
 bool small_backward(uint64_t rows) {
     return rows * sizeof(typename E::raw) <= 2048;
